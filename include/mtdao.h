@@ -477,6 +477,186 @@ int mtdao_set_step(mtdao_handle h, int64_t step);
  */
 const char *mtdao_last_error(mtdao_handle h);
 
+/* ------------------------------------------------------------------ AdamW on tensor lists
+ *
+ * Local AdamW: each of M workers takes AdamW steps on tensors of its own, and
+ * the workers' parameters and states are averaged when the caller's schedule
+ * says so (the base optimizer with decoupled weight decay in place of
+ * Algorithm 1's; one momentum).  Unlike the handle above, the parameters and
+ * gradients stay where the caller has them: M lists of n_tensors device
+ * tensors, fp32 or bf16 each, found by pointer.  The library owns m and v, in
+ * 32 bits or in 8.
+ *
+ * One step of an element, t the 0-based step and s the replica's clip factor
+ * (1 without clipping):
+ *   g' = s g
+ *   m  = beta1 m + (1 - beta1) g'          v = beta2 v + (1 - beta2) g'^2
+ *   p  = p (1 - lr weight_decay decay_k)
+ *        - lr (m / (1 - beta1^(t+1))) / (sqrt(v / (1 - beta2^(t+1))) + eps)
+ * computed in fp32 (square root and quotient to 2 units in the last place).
+ *
+ * State vectors: tensor k starts at a multiple of MTDAO_ADAMW_BLOCK elements
+ * (numels rounded up), so that a block of that many elements belongs to one
+ * tensor; n_state is the sum of the rounded numels, and replica r's vector is
+ * elements r * n_state to (r + 1) * n_state.  In 8 bits every block has a
+ * scale of its own, a power of two: m is e4m3 x scale, with the block's
+ * largest |m| in [128, 256) x scale, v is e5m2 x scale, with its largest in
+ * [2^14, 2^15) x scale.  (e5m2 has in sqrt(v) the resolution that e4m3 has in
+ * m.)  v's code is at least 2^-16 in a block that is not all zero, so that
+ * no m is divided by eps alone because its v was small beside its block's.  A
+ * block whose largest value is below 2^-110 is held as zero; one that holds a
+ * NaN or an infinity has a NaN for its scale.
+ *
+ * Rounding: what a step stores in fewer than 32 bits (m and v in 8, bf16
+ * parameters) is rounded stochastically, because a step's change is mostly
+ * smaller than half the distance between two codes (0.1 % against 6 to 25 % for
+ * beta = 0.999) and rounding to nearest would undo it every time.  The random
+ * bits are a function of (seed, step, replica, place in the state vector):
+ * SplitMix64's counter form for each group of 8 elements, the words of an
+ * element by a multiplication with 0x9E3779B1^(1 + place in the group).  Equal calls on
+ * equal states give equal bits.  mtdao_adamw_average rounds to nearest.
+ */
+#define MTDAO_ADAMW_BLOCK 256
+
+typedef struct {
+    double beta1, beta2;                /* in [0, 1) */
+    double eps;                         /* 1e-30 <= eps */
+    int32_t state_bits;                 /* 32 or 8 */
+    uint64_t seed;                      /* of the stochastic rounding */
+} mtdao_adamw_config;
+
+typedef struct mtdao_adamw_ctx *mtdao_adamw_handle;
+
+/*
+ * M replicas (1..MTDAO_MAX_REPLICAS) of a list of n_tensors tensors of
+ * numel[k] >= 0 elements (one at least not empty).  decay[k] multiplies the
+ * step's weight decay for tensor k (0 for norm weights and biases, say); NULL:
+ * 1 for every tensor.  m = v = 0, t = 0.  The handle works on cuda_stream and
+ * on the device that is current; the call synchronises that stream.
+ * Errors: MTDAO_ERR_INVALID, MTDAO_ERR_OOM, MTDAO_ERR_CUDA.
+ */
+int mtdao_adamw_create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay,
+                       int32_t n_tensors, void *cuda_stream, mtdao_adamw_handle *out);
+
+/* Waits for the handle's stream and frees what the handle owns; NULL is allowed. */
+void mtdao_adamw_destroy(mtdao_adamw_handle h);
+
+int mtdao_adamw_set_stream(mtdao_adamw_handle h, void *cuda_stream);
+
+/*
+ * The parameters: params[r * n_tensors + k] is the device address of replica
+ * r's tensor k (contiguous, aligned to its element size, NULL only if empty),
+ * dtype[k] an mtdao_dtype.  They must not overlap one another.  The addresses
+ * are used by every later step and average: the tensors stay the caller's and
+ * have to outlive that use.  Errors: MTDAO_ERR_INVALID, MTDAO_ERR_ALIGN,
+ * MTDAO_ERR_CUDA; after a refusal the earlier binding stays.  A new binding
+ * asks for a new one of the gradients.
+ */
+int mtdao_adamw_bind_params(mtdao_adamw_handle h, void *const *params, const int32_t *dtype);
+
+/*
+ * The gradients, in the same order; they may overlap one another but no
+ * parameter (MTDAO_ERR_STATE before the parameters are bound).  Needed before the first step, and again when gradients move.
+ */
+int mtdao_adamw_bind_grads(mtdao_adamw_handle h, const void *const *grads, const int32_t *dtype);
+
+/*
+ * One step of every replica on the bound tensors.  max_norm > 0: the
+ * gradient of each replica is first clipped, s = min(1, max_norm / (||g||_2 +
+ * 1e-6)) over all of its tensors (m and v both follow the clipped gradient);
+ * 0: not clipped.  lr and weight_decay are finite, weight_decay >= 0.
+ * Asynchronous.  Errors: MTDAO_ERR_INVALID, MTDAO_ERR_STATE (nothing
+ * bound), MTDAO_ERR_CUDA.
+ */
+int mtdao_adamw_step(mtdao_adamw_handle h, double lr, double weight_decay, double max_norm);
+
+/* sum g^2 of each replica's bound gradients into out_dev (device, M doubles). */
+int mtdao_adamw_grad_sqnorm(mtdao_adamw_handle h, double *out_dev);
+
+/*
+ * Replace on every replica the masked quantities (bit 0: parameters, 1: m,
+ * 2: v) by their mean over the replicas, formed in fp32 as s_0 plus the mean
+ * of the differences to s_0.  Equal replicas stay as they are, but for a v
+ * code that its block's scale can hold better.
+ */
+int mtdao_adamw_average(mtdao_adamw_handle h, uint32_t mask);
+
+/*
+ * Where a state is held (which: 0 = m, 1 = v), for checkpoints and reports:
+ * *values [M][n_state] (fp32, or one byte an element: e4m3 for m, e5m2 for v), *scales [M][n_state /
+ * MTDAO_ADAMW_BLOCK] fp32 (NULL in 32 bits), *n_state.  Owned by the handle.  Output
+ * pointers may be NULL.
+ */
+int mtdao_adamw_state(mtdao_adamw_handle h, int32_t which, void **values, float **scales, int64_t *n_state);
+
+/* Step counter t (-1 for NULL); set: t >= 0, as when resuming. */
+int64_t mtdao_adamw_get_step(mtdao_adamw_handle h);
+int mtdao_adamw_set_step(mtdao_adamw_handle h, int64_t step);
+
+/* As mtdao_last_error, for this kind of handle. */
+const char *mtdao_adamw_last_error(mtdao_adamw_handle h);
+
+/* ------------------------------------------------------------------ Peri-LN residual update
+ *
+ * What stands between two blocks of a decoder with a norm before and after
+ * each block (the paper's models).  For each row (token), x the residual
+ * stream, f the block's output, norm(z) = (z - mean z) / sqrt(var z + eps)
+ * (MTDAO_NORM_LAYER) or z / sqrt(mean z^2 + eps) (MTDAO_NORM_RMS):
+ *   y = residual_scale x + gate (post_w norm(f) + post_b)
+ *   h = pre_w norm(y) + pre_b
+ * y goes on as the stream, h into the next block.  Everything is computed in
+ * fp32 and rounded once to the outputs' types; h is that of the y before its
+ * rounding.
+ */
+typedef enum { MTDAO_NORM_RMS = 0, MTDAO_NORM_LAYER = 1 } mtdao_norm;
+
+#define MTDAO_PERI_NORM_MAX_D 16384
+
+typedef struct {
+    int64_t rows;                       /* >= 0 */
+    int32_t d;                          /* 1 .. MTDAO_PERI_NORM_MAX_D */
+    int32_t norm;                       /* mtdao_norm */
+    int32_t stream_dtype;               /* mtdao_dtype of x, y, dy, dx: fp32, or that of f */
+    int32_t branch_dtype;               /* of f, h, dh, df */
+    int32_t weight_dtype;               /* of the norms' weights and biases and their gradients */
+    int32_t gate_dtype;                 /* of the gate and its gradient */
+    int64_t gate_rows;                  /* 0: no gate; else it divides rows, and row i has gate
+                                           row i / (rows / gate_rows): 1 for a gate per channel,
+                                           rows for one per element */
+    double eps;                         /* >= 0 */
+    double residual_scale;
+    int64_t ld_x, ld_f, ld_y, ld_h;     /* elements between two rows, >= d */
+    int64_t ld_dy, ld_dh, ld_dx, ld_df; /* the same, of the gradients (backward only) */
+} mtdao_peri_norm;
+
+/*
+ * The forward pass.  Rows are contiguous; every pointer is aligned to its
+ * element size.  post_b, pre_b: both or neither (NULL).  gate is NULL where
+ * gate_rows is 0, else [gate_rows][d], contiguous.  stats: NULL, or [2][rows][2]
+ * floats for the backward pass (of f, then of y: mean, or 0 for RMS, and 1 / sqrt(...)).
+ * No output may overlap an input or another output.  Asynchronous on cuda_stream, on the current device.  Errors:
+ * MTDAO_ERR_INVALID, MTDAO_ERR_ALIGN, MTDAO_ERR_CUDA (mtdao_last_error(NULL)).
+ */
+int mtdao_peri_norm_forward(const mtdao_peri_norm *s, const void *x, const void *f, const void *post_w,
+                            const void *post_b, const void *pre_w, const void *pre_b, const void *gate,
+                            void *y, void *h, float *stats, void *cuda_stream);
+
+/* Bytes of device workspace that the backward pass needs; -1 for arguments that it refuses. */
+int64_t mtdao_peri_norm_workspace(const mtdao_peri_norm *s);
+
+/*
+ * The gradients.  dh and dy are those of h and y (dy NULL: zero), y, f and stats
+ * what the forward pass had.  dx and df get the gradients of x and f;
+ * d_post_w, d_pre_w (and d_post_b, d_pre_b, given exactly where post_b was) those of the weights, [d]; d_gate that of the gate,
+ * [gate_rows][d].  Sums over rows are taken in fp32 in a fixed order.
+ * No output may overlap an input or another output.  workspace: device, 16-byte aligned, of mtdao_peri_norm_workspace bytes.
+ */
+int mtdao_peri_norm_backward(const mtdao_peri_norm *s, const void *dh, const void *dy, const void *y,
+                             const void *f, const float *stats, const void *post_w, const void *post_b,
+                             const void *pre_w, const void *gate, void *dx, void *df, void *d_post_w,
+                             void *d_post_b, void *d_pre_w, void *d_pre_b, void *d_gate, void *workspace,
+                             int64_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,9 @@ BASE_ADAM, BASE_ADOPT, BASE_SGDM = 0, 1, 2
 CLIP_NONE, CLIP_GLOBAL_NORM, CLIP_ELEMENTWISE = 0, 1, 2
 F32, BF16 = 0, 1
 PHASE_ALG1, PHASE_ALG2_LITERAL = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
+ADAMW_BLOCK = 256
+PERI_NORM_MAX_D = 16384
 
 BASES = {"adam": BASE_ADAM, "adopt": BASE_ADOPT, "sgdm": BASE_SGDM}
 CLIPS = {"none": CLIP_NONE, "global_norm": CLIP_GLOBAL_NORM, "elementwise": CLIP_ELEMENTWISE}
@@ -48,6 +51,39 @@ class mtdao_config(ctypes.Structure):
         ("period_u", ctypes.c_int64 * MAX_MOM),
         ("period_v", ctypes.c_int64),
         ("adopt_prev_v", ctypes.c_int32),
+    ]
+
+
+class mtdao_adamw_config(ctypes.Structure):
+    _fields_ = [
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("state_bits", ctypes.c_int32),
+        ("seed", ctypes.c_uint64),
+    ]
+
+
+class mtdao_peri_norm(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("d", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
+        ("stream_dtype", ctypes.c_int32),
+        ("branch_dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("gate_dtype", ctypes.c_int32),
+        ("gate_rows", ctypes.c_int64),
+        ("eps", ctypes.c_double),
+        ("residual_scale", ctypes.c_double),
+        ("ld_x", ctypes.c_int64),
+        ("ld_f", ctypes.c_int64),
+        ("ld_y", ctypes.c_int64),
+        ("ld_h", ctypes.c_int64),
+        ("ld_dy", ctypes.c_int64),
+        ("ld_dh", ctypes.c_int64),
+        ("ld_dx", ctypes.c_int64),
+        ("ld_df", ctypes.c_int64),
     ]
 
 
@@ -106,6 +142,27 @@ def _load():
         "mtdao_get_step": (ctypes.c_int64, [H]),
         "mtdao_set_step": (ctypes.c_int, [H, ctypes.c_int64]),
         "mtdao_last_error": (ctypes.c_char_p, [H]),
+        "mtdao_adamw_create": (ctypes.c_int, [ctypes.POINTER(mtdao_adamw_config), ctypes.c_int32, i64p,
+                                              ctypes.POINTER(ctypes.c_float), ctypes.c_int32, ctypes.c_void_p,
+                                              ctypes.POINTER(H)]),
+        "mtdao_adamw_destroy": (None, [H]),
+        "mtdao_adamw_set_stream": (ctypes.c_int, [H, ctypes.c_void_p]),
+        "mtdao_adamw_bind_params": (ctypes.c_int, [H, ctypes.POINTER(ctypes.c_void_p),
+                                                   ctypes.POINTER(ctypes.c_int32)]),
+        "mtdao_adamw_bind_grads": (ctypes.c_int, [H, ctypes.POINTER(ctypes.c_void_p),
+                                                  ctypes.POINTER(ctypes.c_int32)]),
+        "mtdao_adamw_step": (ctypes.c_int, [H, ctypes.c_double, ctypes.c_double, ctypes.c_double]),
+        "mtdao_adamw_grad_sqnorm": (ctypes.c_int, [H, ctypes.c_void_p]),
+        "mtdao_adamw_average": (ctypes.c_int, [H, ctypes.c_uint32]),
+        "mtdao_adamw_state": (ctypes.c_int, [H, ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p),
+                                             ctypes.POINTER(ctypes.c_void_p), i64p]),
+        "mtdao_adamw_get_step": (ctypes.c_int64, [H]),
+        "mtdao_adamw_set_step": (ctypes.c_int, [H, ctypes.c_int64]),
+        "mtdao_adamw_last_error": (ctypes.c_char_p, [H]),
+        "mtdao_peri_norm_forward": (ctypes.c_int, [ctypes.POINTER(mtdao_peri_norm)] + [ctypes.c_void_p] * 11),
+        "mtdao_peri_norm_workspace": (ctypes.c_int64, [ctypes.POINTER(mtdao_peri_norm)]),
+        "mtdao_peri_norm_backward": (ctypes.c_int, [ctypes.POINTER(mtdao_peri_norm)] + [ctypes.c_void_p] * 16
+                                     + [ctypes.c_int64, ctypes.c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -325,6 +382,111 @@ def mtdao_set_step(h, step: int) -> None:
 
 def mtdao_last_error(h=None) -> str:
     return (lib.mtdao_last_error(h) or b"").decode()
+
+
+# AdamW on tensor lists and the Peri-LN residual update: wrappers of the C
+# calls, and the classes and functions that take torch tensors (adamw.py,
+# norms.py), imported on first use because they need torch.
+
+def _check_adamw(rc, h):
+    if rc != OK:
+        raise MTDAOError(rc, (lib.mtdao_adamw_last_error(h) or b"").decode())
+    return rc
+
+
+def mtdao_adamw_create(cfg: mtdao_adamw_config, M: int, numels, decay=None, stream: int = 0):
+    n = len(numels)
+    arr = (ctypes.c_int64 * n)(*[int(k) for k in numels])
+    dec = None if decay is None else (ctypes.c_float * n)(*[float(k) for k in decay])
+    h = ctypes.c_void_p()
+    _check(lib.mtdao_adamw_create(ctypes.byref(cfg), M, arr, dec, n, ctypes.c_void_p(stream), ctypes.byref(h)))
+    return h
+
+
+def mtdao_adamw_destroy(h) -> None:
+    lib.mtdao_adamw_destroy(h)
+
+
+def mtdao_adamw_set_stream(h, stream: int) -> None:
+    _check_adamw(lib.mtdao_adamw_set_stream(h, ctypes.c_void_p(stream)), h)
+
+
+def _address_table(ptrs, dtypes):
+    return ((ctypes.c_void_p * len(ptrs))(*[int(p) or None for p in ptrs]),
+            (ctypes.c_int32 * len(dtypes))(*dtypes))
+
+
+def mtdao_adamw_bind_params(h, ptrs, dtypes) -> None:
+    """ptrs: device addresses, M * n_tensors of them; dtypes: n_tensors codes."""
+    _check_adamw(lib.mtdao_adamw_bind_params(h, *_address_table(ptrs, dtypes)), h)
+
+
+def mtdao_adamw_bind_grads(h, ptrs, dtypes) -> None:
+    _check_adamw(lib.mtdao_adamw_bind_grads(h, *_address_table(ptrs, dtypes)), h)
+
+
+def mtdao_adamw_step(h, lr: float, weight_decay: float = 0.0, max_norm: float = 0.0) -> None:
+    _check_adamw(lib.mtdao_adamw_step(h, lr, weight_decay, max_norm), h)
+
+
+def mtdao_adamw_grad_sqnorm(h, out_dev_ptr: int) -> None:
+    _check_adamw(lib.mtdao_adamw_grad_sqnorm(h, ctypes.c_void_p(out_dev_ptr)), h)
+
+
+def mtdao_adamw_average(h, mask: int) -> None:
+    _check_adamw(lib.mtdao_adamw_average(h, mask), h)
+
+
+def mtdao_adamw_state(h, which: int):
+    """(address of the values, address of the scales or None, n_state)"""
+    v, s, n = ctypes.c_void_p(), ctypes.c_void_p(), ctypes.c_int64()
+    _check_adamw(lib.mtdao_adamw_state(h, which, ctypes.byref(v), ctypes.byref(s), ctypes.byref(n)), h)
+    return v.value, s.value, int(n.value)
+
+
+def mtdao_adamw_get_step(h) -> int:
+    return int(lib.mtdao_adamw_get_step(h))
+
+
+def mtdao_adamw_set_step(h, step: int) -> None:
+    _check_adamw(lib.mtdao_adamw_set_step(h, int(step)), h)
+
+
+def mtdao_peri_norm_forward(shape: mtdao_peri_norm, x, f, post_w, post_b, pre_w, pre_b, gate, y, h, stats,
+                            stream: int = 0) -> None:
+    """Device addresses (None for what is left out)."""
+    _check(lib.mtdao_peri_norm_forward(ctypes.byref(shape), x, f, post_w, post_b, pre_w, pre_b, gate, y, h, stats,
+                                       stream))
+
+
+def mtdao_peri_norm_workspace(shape: mtdao_peri_norm) -> int:
+    n = int(lib.mtdao_peri_norm_workspace(ctypes.byref(shape)))
+    if n < 0:
+        _check(ERR_INVALID)
+    return n
+
+
+def mtdao_peri_norm_backward(shape: mtdao_peri_norm, dh, dy, y, f, stats, post_w, post_b, pre_w, gate, dx, df,
+                             d_post_w, d_post_b, d_pre_w, d_pre_b, d_gate, workspace, workspace_bytes: int,
+                             stream: int = 0) -> None:
+    _check(lib.mtdao_peri_norm_backward(ctypes.byref(shape), dh, dy, y, f, stats, post_w, post_b, pre_w, gate, dx,
+                                        df, d_post_w, d_post_b, d_pre_w, d_pre_b, d_gate, workspace,
+                                        workspace_bytes, stream))
+
+
+_LAZY = {"AdamW": "adamw", "peri_norm": "norms", "peri_norm_forward": "norms",
+         "peri_norm_backward": "norms"}
+
+
+def __getattr__(name):
+    if name not in _LAZY:
+        raise AttributeError("module %r has no attribute %r" % (__name__, name))
+    import importlib
+    module = importlib.import_module("." + _LAZY[name], __name__)
+    for known, where in _LAZY.items():
+        if where == _LAZY[name]:
+            globals()[known] = getattr(module, known)
+    return globals()[name]
 
 
 class MTDAO:

@@ -1,0 +1,154 @@
+"""AdamW for M worker replicas of a list of tensors (``mtdao_adamw_*`` of
+``include/mtdao.h``), on torch tensors."""
+from __future__ import annotations
+
+import torch
+
+import paper_2510_05361_gb300 as P
+
+_CODES = {torch.float32: P.F32, torch.bfloat16: P.BF16}
+_STATES = {"m": (0, torch.float8_e4m3fn), "v": (1, torch.float8_e5m2)}
+PARAMS, M_STATE, V_STATE = 1, 2, 4           # bits of average()'s mask
+
+
+class AdamW:
+    """Owning wrapper of one handle.
+
+    ``params``: the tensors of one model (a list), or one such list for each of
+    M worker replicas; fp32 or bf16, contiguous, all on one GPU.  ``grads``: the
+    gradients in the same nesting, in buffers that stay where they are (``bind_grads``
+    gives new ones).  ``state_bits``: 32, or 8 for m and v in blocks of 256 with a
+    scale each and stochastic rounding from ``seed``.  ``decay``: a factor of the
+    weight decay for each tensor (0 exempts it).  The handle works on torch's
+    current stream at construction unless another is given.
+    """
+
+    def __init__(self, params, grads=None, *, betas=(0.9, 0.999), eps: float = 1e-8, state_bits: int = 32,
+                 decay=None, seed: int = 0, stream: int | None = None):
+        self._h = None
+        params = self._nested(params, "params")
+        self.M = len(params)
+        self.numels = [int(t.numel()) for t in params[0]]
+        if decay is not None and len(decay) != len(self.numels):
+            raise ValueError("expected %d decay factors, got %d" % (len(self.numels), len(decay)))
+        self.state_bits = int(state_bits)
+        first = next((t for t in params[0]), None)
+        if first is None or not first.is_cuda:
+            raise ValueError("params must be in device memory")
+        self.device = first.device
+        codes = self._check(params, "params")
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device).cuda_stream
+        cfg = P.mtdao_adamw_config(float(betas[0]), float(betas[1]), float(eps), self.state_bits,
+                                   int(seed) % (1 << 64))
+        with torch.cuda.device(self.device):
+            self._h = P.mtdao_adamw_create(cfg, self.M, self.numels, decay, stream)
+            P.mtdao_adamw_bind_params(self._h, [t.data_ptr() for row in params for t in row], codes)
+        self.params, self.grads = params, None
+        if grads is not None:
+            self.bind_grads(grads)
+
+    @property
+    def h(self):
+        if self._h is None:
+            raise P.MTDAOError(P.ERR_STATE, "the optimizer is closed")
+        return self._h
+
+    def close(self) -> None:
+        if self._h is not None:
+            P.mtdao_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @staticmethod
+    def _nested(tensors, what):
+        tensors = list(tensors)
+        if not tensors:
+            raise ValueError("%s: empty list" % what)
+        if isinstance(tensors[0], torch.Tensor):
+            tensors = [tensors]
+        return [list(row) for row in tensors]
+
+    def _check(self, rows, what):
+        """The tensors are passed by address: their layout must be the one that
+        the library reads.  Returns the type codes, one a tensor."""
+        if len(rows) != self.M or any(len(row) != len(self.numels) for row in rows):
+            raise ValueError("%s: expected %d lists of %d tensors" % (what, self.M, len(self.numels)))
+        codes = []
+        for k, first in enumerate(rows[0]):
+            if first.dtype not in _CODES:
+                raise ValueError("%s: dtype %s not supported" % (what, first.dtype))
+            codes.append(_CODES[first.dtype])
+            for row in rows:
+                t = row[k]
+                if t.numel() != self.numels[k]:
+                    raise ValueError("%s: tensor %d has %d elements, expected %d" % (what, k, t.numel(), self.numels[k]))
+                if t.dtype != first.dtype:
+                    raise ValueError("%s: tensor %d differs in dtype between replicas" % (what, k))
+                if not t.is_contiguous():
+                    raise ValueError("%s: tensor %d must be contiguous" % (what, k))
+                if t.device != self.device:
+                    raise ValueError("%s: tensor %d must be on %s" % (what, k, self.device))
+        return codes
+
+    def bind_grads(self, grads) -> None:
+        """The gradients of every later step: the buffers themselves, not their values now."""
+        grads = self._nested(grads, "grads")
+        codes = self._check(grads, "grads")
+        P.mtdao_adamw_bind_grads(self.h, [t.data_ptr() for row in grads for t in row], codes)
+        self.grads = grads
+
+    def step(self, lr: float, weight_decay: float = 0.0, max_norm: float | None = None) -> None:
+        """One step of every replica; ``max_norm`` clips each replica's gradient first."""
+        if max_norm is not None and not max_norm > 0.0:
+            raise ValueError("max_norm must be positive, or None")
+        h = self.h
+        rc = P.lib.mtdao_adamw_step(h, lr, weight_decay, 0.0 if max_norm is None else max_norm)
+        if rc:
+            P._check_adamw(rc, h)
+
+    def average(self, mask: int = PARAMS | M_STATE | V_STATE) -> None:
+        """Replaces parameters (1), m (2) and v (4) by their means over the replicas."""
+        P.mtdao_adamw_average(self.h, mask)
+
+    def grad_sqnorm(self):
+        """Sum of squares of each replica's bound gradients, [M] fp64 on the device."""
+        out = torch.empty((self.M,), dtype=torch.float64, device=self.device)
+        P.mtdao_adamw_grad_sqnorm(self.h, out.data_ptr())
+        return out
+
+    def state(self, name: str):
+        """The memory of "m" or "v": [M][n_state] fp32, or in 8 bits
+        ``{"codes": [M][n_state] float8, "scales": [M][n_state / 256] fp32}`` (a value is
+        its code times its block's scale).  Valid until ``close``; the views keep
+        this object."""
+        which, kind = _STATES[name]
+        values, scales, n = P.mtdao_adamw_state(self.h, which)
+        if self.state_bits == 32:
+            return self._view(values, (self.M, n), "<f4")
+        return {"codes": self._view(values, (self.M, n), "|u1").view(kind),
+                "scales": self._view(scales, (self.M, n // P.ADAMW_BLOCK), "<f4")}
+
+    def _view(self, ptr, shape, typestr):
+        class Memory:
+            def __init__(self, owner):
+                self.owner = owner
+                self.__cuda_array_interface__ = {"shape": shape, "typestr": typestr, "data": (ptr, False),
+                                                 "version": 3, "strides": None}
+        return torch.as_tensor(Memory(self), device=self.device)
+
+    def set_stream(self, stream: int) -> None:
+        P.mtdao_adamw_set_stream(self.h, stream)
+
+    @property
+    def t(self) -> int:
+        return P.mtdao_adamw_get_step(self.h)
+
+    @t.setter
+    def t(self, value: int) -> None:
+        P.mtdao_adamw_set_step(self.h, value)

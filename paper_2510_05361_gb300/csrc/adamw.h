@@ -1,0 +1,70 @@
+// adamw.h -- shared between the AdamW host code and its kernels.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "mtdao.h"
+
+namespace mtdao {
+
+constexpr int kAdamwBlock = MTDAO_ADAMW_BLOCK;   // elements that share a scale: one warp's
+constexpr int kAdamwChunk = 2048;                // elements of one record: one thread block's
+constexpr int kAdamwThreads = 256;
+
+// A stretch of one tensor of one replica, as the kernels walk the list: up to
+// kAdamwChunk elements, so that a thread block finds its addresses with one
+// load of 32 bytes (0.2 % of what a step moves).
+struct __align__(16) AdamwChunk {
+    void *p;                  // first element of the parameters
+    const void *g;            // and of the gradients
+    uint32_t block;           // its first state block, counted over all replicas
+    int32_t n;                // 1 .. kAdamwChunk elements
+    uint32_t flags;           // kAdamw*
+    float decay;              // the tensor's decay factor
+};
+constexpr uint32_t kAdamwParamBf16 = 1, kAdamwGradBf16 = 2;
+
+// What does not depend on the step.
+struct AdamwList {
+    const AdamwChunk *chunks;    // [M][n_chunks]
+    int64_t n_chunks;            // of one replica
+    int64_t n_state;             // elements of one replica's state vector
+    int32_t M;
+    int32_t bits;                // 32 or 8
+    void *m, *v;                 // [M][n_state] fp32, e4m3 and e5m2 in 8 bits
+    float *m_scale, *v_scale;    // [M][n_state / kAdamwBlock]
+};
+
+struct AdamwScalars {
+    float b1, c1, b2, c2;        // beta, 1 - beta
+    float step;                  // lr / (1 - beta1^(t+1))
+    float root;                  // 1 / sqrt(1 - beta2^(t+1))
+    float eps;
+    float decay;                 // lr * weight_decay
+    uint64_t key;                // of (seed, step): the stochastic rounding's counter starts here
+};
+
+// A tensor of the list, the same for every replica.
+struct AdamwTensor {
+    int64_t numel;
+    int64_t first_chunk, first_block;    // of one replica
+    float decay;
+    int32_t pad;
+};
+
+// Writes the addresses in table [M][n_tensors] (and what else belongs to the parameters) into the records.
+cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, int32_t n_tensors, void *const *table,
+                              const int32_t *dtype, bool grads, int64_t n_chunks, int64_t n_blocks, int32_t M,
+                              cudaStream_t stream);
+cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream);
+
+// ||g||^2 of each replica into sums[M] (fixed order) and, where scale is not
+// NULL, min(1, max_norm / (||g|| + 1e-6)) into scale[M].  partial holds M *
+// adamw_norm_blocks() doubles.
+int adamw_norm_blocks(int num_sms, int M, int64_t n_chunks);
+cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, double *sums, float *scale,
+                              double max_norm, cudaStream_t stream);
+cudaError_t launch_adamw_average(const AdamwList &a, uint32_t mask, cudaStream_t stream);
+
+}  // namespace mtdao

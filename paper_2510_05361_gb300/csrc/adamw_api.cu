@@ -1,0 +1,362 @@
+// adamw_api.cu -- host side of the AdamW calls declared in include/mtdao.h:
+// checks of arguments, the list's layout, the step's scalars (in double,
+// rounded once), device memory and launches.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <cstdint>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include <nvtx3/nvToolsExt.h>
+
+#include "adamw.h"
+#include "adamw_codes.cuh"
+#include "mtdao_internal.h"
+
+using namespace mtdao;
+
+struct mtdao_adamw_ctx {
+    mtdao_adamw_config cfg;
+    int32_t n_tensors = 0;
+    std::vector<AdamwTensor> tensors;
+    AdamwList list = {};
+    AdamwChunk *chunks = nullptr;
+    AdamwTensor *tensors_dev = nullptr;
+    void **table = nullptr;              // [M][n_tensors], scratch of a binding
+    int32_t *dtypes = nullptr;           // [n_tensors], likewise
+    int norm_blocks = 1;
+    double *norm_partial = nullptr, *norm_sums = nullptr;
+    float *clip_scale = nullptr;
+    int device = 0;
+    cudaStream_t stream = nullptr;
+    int64_t step = 0;
+    bool has_params = false, has_grads = false;
+    std::vector<std::pair<uintptr_t, uintptr_t>> spans;    // of the bound parameters, sorted
+    char err[512] = "";
+};
+
+namespace {
+
+struct Range {
+    explicit Range(const char *name) { nvtxRangePushA(name); }
+    ~Range() { nvtxRangePop(); }
+    Range(const Range &) = delete;
+    Range &operator=(const Range &) = delete;
+};
+
+// The message goes to the handle, or to the thread where there is none.
+int fail(mtdao_adamw_ctx *h, int code, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    if (h == nullptr) return set_thread_error(code, buf);
+    std::memcpy(h->err, buf, sizeof buf);
+    return code;
+}
+int cuda_fail(mtdao_adamw_ctx *h, cudaError_t e, const char *what) {
+    return fail(h, MTDAO_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+int select_device(mtdao_adamw_ctx *h) {
+    int cur = -1;
+    cudaError_t e = cudaGetDevice(&cur);
+    if (e == cudaSuccess && cur != h->device) e = cudaSetDevice(h->device);
+    return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "selecting the handle's device");
+}
+
+void release(mtdao_adamw_ctx *h) {
+    cudaStreamSynchronize(h->stream);
+    void *owned[] = {h->list.m, h->list.v, h->list.m_scale, h->list.v_scale, h->chunks, h->tensors_dev,
+                     h->table, h->dtypes, h->norm_partial, h->norm_sums, h->clip_scale};
+    for (void *p : owned)
+        if (p) cudaFree(p);
+}
+
+bool rate(double b) { return b >= 0.0 && b < 1.0; }
+
+int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay, int32_t n_tensors,
+           void *cuda_stream, mtdao_adamw_ctx *h) {
+    h->cfg = *cfg;
+    h->n_tensors = n_tensors;
+    h->tensors.resize(n_tensors);
+    int64_t chunks = 0, blocks = 0;
+    for (int32_t k = 0; k < n_tensors; ++k) {
+        if (numel[k] < 0 || numel[k] > (int64_t(1) << 40))
+            return fail(nullptr, MTDAO_ERR_INVALID, "tensor %d has numel %lld", k, static_cast<long long>(numel[k]));
+        const float d = decay ? decay[k] : 1.0f;
+        if (!(std::isfinite(d) && d >= 0.0f))
+            return fail(nullptr, MTDAO_ERR_INVALID, "decay[%d]=%g must be finite and not negative", k, d);
+        h->tensors[k] = {numel[k], chunks, blocks, d, 0};
+        chunks += (numel[k] + kAdamwChunk - 1) / kAdamwChunk;
+        blocks += (numel[k] + kAdamwBlock - 1) / kAdamwBlock;
+        if (blocks > 0xffffffffll) break;
+    }
+    if (blocks == 0) return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list holds no element");
+    // the records count blocks in 32 bits, the launches chunks in 31, the random numbers groups of 8 in 32
+    if (blocks * M > 0xffffffffll || chunks * M > 0x7fffffffll || blocks * (kAdamwBlock / 8) > 0xffffffffll)
+        return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list is too long for %d replicas", M);
+
+    h->stream = static_cast<cudaStream_t>(cuda_stream);
+    int sms = 1;
+    cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
+    if (e != cudaSuccess) return cuda_fail(nullptr, e, "no usable CUDA device");
+
+    AdamwList &a = h->list;
+    a.M = M;
+    a.bits = cfg->state_bits;
+    a.n_chunks = chunks;
+    a.n_state = blocks * kAdamwBlock;
+    h->norm_blocks = adamw_norm_blocks(sms, M, chunks);
+    const size_t held = static_cast<size_t>(M) * a.n_state * (a.bits / 8);
+    const size_t scales = a.bits == 8 ? static_cast<size_t>(M) * blocks * sizeof(float) : 0;
+    struct {
+        void **p;
+        size_t bytes;
+        const char *what;
+    } allocs[] = {
+        {&a.m, held, "m"},
+        {&a.v, held, "v"},
+        {reinterpret_cast<void **>(&a.m_scale), scales, "m's scales"},
+        {reinterpret_cast<void **>(&a.v_scale), scales, "v's scales"},
+        {reinterpret_cast<void **>(&h->chunks), static_cast<size_t>(M) * chunks * sizeof(AdamwChunk), "records"},
+        {reinterpret_cast<void **>(&h->tensors_dev), n_tensors * sizeof(AdamwTensor), "tensor list"},
+        {reinterpret_cast<void **>(&h->table), static_cast<size_t>(M) * n_tensors * sizeof(void *), "address table"},
+        {reinterpret_cast<void **>(&h->dtypes), n_tensors * sizeof(int32_t), "type table"},
+        {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(M) * h->norm_blocks * sizeof(double),
+         "norm partials"},
+        {reinterpret_cast<void **>(&h->norm_sums), M * sizeof(double), "norms"},
+        {reinterpret_cast<void **>(&h->clip_scale), M * sizeof(float), "clip factors"},
+    };
+    for (auto &x : allocs) {
+        if (x.bytes == 0) continue;
+        e = cudaMalloc(x.p, x.bytes);
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            *x.p = nullptr;
+            return fail(nullptr, MTDAO_ERR_OOM, "cudaMalloc of %s (%zu bytes) failed: %s", x.what, x.bytes,
+                        cudaGetErrorString(e));
+        }
+    }
+    a.chunks = h->chunks;
+    e = cudaMemsetAsync(a.m, 0, held, h->stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(a.v, 0, held, h->stream);
+    if (e == cudaSuccess && scales) e = cudaMemsetAsync(a.m_scale, 0, scales, h->stream);
+    if (e == cudaSuccess && scales) e = cudaMemsetAsync(a.v_scale, 0, scales, h->stream);
+    if (e == cudaSuccess)
+        e = cudaMemsetAsync(h->chunks, 0, static_cast<size_t>(M) * chunks * sizeof(AdamwChunk), h->stream);
+    if (e == cudaSuccess)
+        e = cudaMemcpyAsync(h->tensors_dev, h->tensors.data(), n_tensors * sizeof(AdamwTensor), cudaMemcpyHostToDevice,
+                            h->stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(h->stream);
+    return e == cudaSuccess ? MTDAO_OK : cuda_fail(nullptr, e, "setting up the states");
+}
+
+// Checks a table of addresses, [M][n_tensors], and gives the spans that it covers.
+int spans_of(mtdao_adamw_ctx *h, void *const *table, const int32_t *dtype, const char *what,
+             std::vector<std::pair<uintptr_t, uintptr_t>> &spans) {
+    if (table == nullptr || dtype == nullptr) return fail(h, MTDAO_ERR_INVALID, "%s: NULL table", what);
+    for (int32_t k = 0; k < h->n_tensors; ++k) {
+        if (dtype[k] != MTDAO_F32 && dtype[k] != MTDAO_BF16)
+            return fail(h, MTDAO_ERR_INVALID, "%s: unknown type %d of tensor %d", what, dtype[k], k);
+        const uintptr_t size = dtype[k] == MTDAO_BF16 ? 2 : 4;
+        if (h->tensors[k].numel == 0) continue;
+        for (int32_t r = 0; r < h->list.M; ++r) {
+            const uintptr_t p = reinterpret_cast<uintptr_t>(table[static_cast<size_t>(r) * h->n_tensors + k]);
+            if (p == 0) return fail(h, MTDAO_ERR_INVALID, "%s: tensor %d of replica %d is NULL", what, k, r);
+            if (p % size) return fail(h, MTDAO_ERR_ALIGN, "%s: tensor %d of replica %d is not aligned to its type", what, k, r);
+            spans.emplace_back(p, p + h->tensors[k].numel * size);
+        }
+    }
+    std::sort(spans.begin(), spans.end());
+    return MTDAO_OK;
+}
+
+int upload(mtdao_adamw_ctx *h, void *const *table, const int32_t *dtype, bool grads) {
+    const AdamwList &a = h->list;
+    cudaError_t e = cudaMemcpyAsync(h->table, table, static_cast<size_t>(a.M) * h->n_tensors * sizeof(void *),
+                                    cudaMemcpyHostToDevice, h->stream);
+    if (e == cudaSuccess)
+        e = cudaMemcpyAsync(h->dtypes, dtype, h->n_tensors * sizeof(int32_t), cudaMemcpyHostToDevice, h->stream);
+    if (e == cudaSuccess)
+        e = launch_adamw_bind(h->chunks, h->tensors_dev, h->n_tensors, h->table, h->dtypes, grads, a.n_chunks,
+                              a.n_state / kAdamwBlock, a.M, h->stream);
+    return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "binding tensors");
+}
+
+int no_handle() { return set_thread_error(MTDAO_ERR_INVALID, "handle is NULL"); }
+
+}  // namespace
+
+extern "C" int mtdao_adamw_create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay,
+                                  int32_t n_tensors, void *cuda_stream, mtdao_adamw_handle *out) {
+    if (out == nullptr) return set_thread_error(MTDAO_ERR_INVALID, "out is NULL");
+    *out = nullptr;
+    if (cfg == nullptr) return set_thread_error(MTDAO_ERR_INVALID, "config is NULL");
+    if (!rate(cfg->beta1) || !rate(cfg->beta2))
+        return fail(nullptr, MTDAO_ERR_INVALID, "beta1=%g, beta2=%g must lie in [0,1)", cfg->beta1, cfg->beta2);
+    if (!(std::isfinite(cfg->eps) && cfg->eps >= 1e-30))
+        return fail(nullptr, MTDAO_ERR_INVALID, "eps=%g must be at least 1e-30", cfg->eps);
+    if (cfg->state_bits != 8 && cfg->state_bits != 32)
+        return fail(nullptr, MTDAO_ERR_INVALID, "state_bits=%d must be 8 or 32", cfg->state_bits);
+    if (M < 1 || M > MTDAO_MAX_REPLICAS)
+        return fail(nullptr, MTDAO_ERR_INVALID, "M %d outside 1..%d", M, MTDAO_MAX_REPLICAS);
+    if (numel == nullptr || n_tensors < 1) return set_thread_error(MTDAO_ERR_INVALID, "empty tensor list");
+    mtdao_adamw_ctx *h = nullptr;
+    int rc;
+    try {
+        h = new mtdao_adamw_ctx();
+        rc = create(cfg, M, numel, decay, n_tensors, cuda_stream, h);
+    } catch (const std::bad_alloc &) {
+        rc = set_thread_error(MTDAO_ERR_OOM, "out of host memory");
+    }
+    if (rc == MTDAO_OK) {
+        *out = h;
+    } else if (h != nullptr) {
+        release(h);
+        delete h;
+    }
+    return rc;
+}
+
+extern "C" void mtdao_adamw_destroy(mtdao_adamw_handle h) {
+    if (h == nullptr) return;
+    int cur = -1;
+    if (cudaGetDevice(&cur) == cudaSuccess && cur != h->device) cudaSetDevice(h->device);
+    release(h);
+    if (cur >= 0 && cur != h->device) cudaSetDevice(cur);
+    delete h;
+}
+
+extern "C" int mtdao_adamw_set_stream(mtdao_adamw_handle h, void *cuda_stream) {
+    if (h == nullptr) return no_handle();
+    h->stream = static_cast<cudaStream_t>(cuda_stream);
+    return MTDAO_OK;
+}
+
+extern "C" int mtdao_adamw_bind_params(mtdao_adamw_handle h, void *const *params, const int32_t *dtype) {
+    if (h == nullptr) return no_handle();
+    Range range("mtdao_adamw_bind_params");
+    try {
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        if (int rc = spans_of(h, params, dtype, "params", spans)) return rc;
+        for (size_t i = 1; i < spans.size(); ++i)
+            if (spans[i].first < spans[i - 1].second)
+                return fail(h, MTDAO_ERR_INVALID, "params: two tensors overlap");
+        if (int rc = select_device(h)) return rc;
+        h->has_params = h->has_grads = false;      // the gradients were checked against the earlier parameters
+        if (int rc = upload(h, params, dtype, false)) return rc;
+        h->spans.swap(spans);
+        h->has_params = true;
+        return MTDAO_OK;
+    } catch (const std::bad_alloc &) {
+        return fail(h, MTDAO_ERR_OOM, "out of host memory");
+    }
+}
+
+extern "C" int mtdao_adamw_bind_grads(mtdao_adamw_handle h, const void *const *grads, const int32_t *dtype) {
+    if (h == nullptr) return no_handle();
+    if (!h->has_params) return fail(h, MTDAO_ERR_STATE, "grads: the parameters are not bound");
+    Range range("mtdao_adamw_bind_grads");
+    try {
+        void *const *table = const_cast<void *const *>(grads);
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        if (int rc = spans_of(h, table, dtype, "grads", spans)) return rc;
+        // both lists are sorted, the parameters' spans disjoint
+        size_t i = 0;
+        for (const auto &g : spans) {
+            while (i < h->spans.size() && h->spans[i].second <= g.first) ++i;
+            if (i < h->spans.size() && h->spans[i].first < g.second)
+                return fail(h, MTDAO_ERR_INVALID, "grads: a tensor overlaps a parameter");
+        }
+        if (int rc = select_device(h)) return rc;
+        h->has_grads = false;
+        if (int rc = upload(h, table, dtype, true)) return rc;
+        h->has_grads = true;
+        return MTDAO_OK;
+    } catch (const std::bad_alloc &) {
+        return fail(h, MTDAO_ERR_OOM, "out of host memory");
+    }
+}
+
+extern "C" int mtdao_adamw_step(mtdao_adamw_handle h, double lr, double weight_decay, double max_norm) {
+    if (h == nullptr) return no_handle();
+    if (!std::isfinite(lr) || !(std::isfinite(weight_decay) && weight_decay >= 0.0) ||
+        !(std::isfinite(max_norm) && max_norm >= 0.0))
+        return fail(h, MTDAO_ERR_INVALID, "lr=%g, weight_decay=%g, max_norm=%g: finite values wanted, the latter two not negative",
+                    lr, weight_decay, max_norm);
+    if (!h->has_params || !h->has_grads) return fail(h, MTDAO_ERR_STATE, "step: no parameters or gradients are bound");
+    Range range("mtdao_adamw_step");
+    if (int rc = select_device(h)) return rc;
+    const mtdao_adamw_config &c = h->cfg;
+    const double t = static_cast<double>(h->step + 1);
+    AdamwScalars sc;
+    sc.b1 = static_cast<float>(c.beta1);
+    sc.c1 = static_cast<float>(1.0 - c.beta1);
+    sc.b2 = static_cast<float>(c.beta2);
+    sc.c2 = static_cast<float>(1.0 - c.beta2);
+    sc.step = static_cast<float>(lr / (1.0 - std::pow(c.beta1, t)));
+    sc.root = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(c.beta2, t)));
+    sc.eps = static_cast<float>(c.eps);
+    sc.decay = static_cast<float>(lr * weight_decay);
+    sc.key = splitmix64(c.seed + kGolden * (static_cast<uint64_t>(h->step) + 1));
+    const float *scale = nullptr;
+    cudaError_t e = cudaSuccess;
+    if (max_norm > 0.0) {
+        scale = h->clip_scale;
+        e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, h->norm_sums, h->clip_scale, max_norm, h->stream);
+    }
+    if (e == cudaSuccess) e = launch_adamw_step(h->list, sc, scale, h->stream);
+    if (e != cudaSuccess) return cuda_fail(h, e, "AdamW step");
+    ++h->step;
+    return MTDAO_OK;
+}
+
+extern "C" int mtdao_adamw_grad_sqnorm(mtdao_adamw_handle h, double *out_dev) {
+    if (h == nullptr) return no_handle();
+    if (out_dev == nullptr) return fail(h, MTDAO_ERR_INVALID, "out is NULL");
+    if (reinterpret_cast<uintptr_t>(out_dev) & 7u) return fail(h, MTDAO_ERR_ALIGN, "out not 8-byte aligned");
+    if (!h->has_grads) return fail(h, MTDAO_ERR_STATE, "grad_sqnorm: no gradients are bound");
+    Range range("mtdao_adamw_grad_sqnorm");
+    if (int rc = select_device(h)) return rc;
+    const cudaError_t e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, out_dev, nullptr, 0.0, h->stream);
+    return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "gradient norm");
+}
+
+extern "C" int mtdao_adamw_average(mtdao_adamw_handle h, uint32_t mask) {
+    if (h == nullptr) return no_handle();
+    if (mask & ~7u) return fail(h, MTDAO_ERR_INVALID, "average: mask 0x%x has unknown bits", mask);
+    if (!h->has_params) return fail(h, MTDAO_ERR_STATE, "average: the parameters are not bound");
+    if (mask == 0 || h->list.M == 1) return MTDAO_OK;
+    Range range("mtdao_adamw_average");
+    if (int rc = select_device(h)) return rc;
+    const cudaError_t e = launch_adamw_average(h->list, mask, h->stream);
+    return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "average");
+}
+
+extern "C" int mtdao_adamw_state(mtdao_adamw_handle h, int32_t which, void **values, float **scales, int64_t *n_state) {
+    if (h == nullptr) return no_handle();
+    if (which != 0 && which != 1) return fail(h, MTDAO_ERR_INVALID, "state %d: 0 (m) or 1 (v)", which);
+    if (values) *values = which == 0 ? h->list.m : h->list.v;
+    if (scales) *scales = which == 0 ? h->list.m_scale : h->list.v_scale;
+    if (n_state) *n_state = h->list.n_state;
+    return MTDAO_OK;
+}
+
+extern "C" int mtdao_adamw_set_step(mtdao_adamw_handle h, int64_t step) {
+    if (h == nullptr) return no_handle();
+    if (step < 0) return fail(h, MTDAO_ERR_INVALID, "step must not be negative");
+    h->step = step;
+    return MTDAO_OK;
+}
+
+extern "C" int64_t mtdao_adamw_get_step(mtdao_adamw_handle h) { return h ? h->step : -1; }
+
+extern "C" const char *mtdao_adamw_last_error(mtdao_adamw_handle h) { return h ? h->err : mtdao_last_error(nullptr); }
