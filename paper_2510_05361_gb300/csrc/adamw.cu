@@ -24,26 +24,104 @@ __device__ __forceinline__ AdamwChunk load_chunk(const AdamwChunk *c) {
     return u.chunk;
 }
 
-__device__ __forceinline__ float bf16_to_float(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
+// Eight consecutive 32-bit words of a lane in one access of 32 bytes, streamed past the caches:
+// everything is read once and written once.
+__device__ __forceinline__ void load_words8(const void *p, uint32_t *w) {
+    asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store_words8(void *p, const uint32_t *w) {
+    asm volatile("st.global.cs.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 :: "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void load_f32x8(const float *p, float *x) { load_words8(p, reinterpret_cast<uint32_t *>(x)); }
+__device__ __forceinline__ void store_f32x8(float *p, const float *x) {
+    store_words8(p, reinterpret_cast<const uint32_t *>(x));
+}
 
-// Eight values of a tensor from element at on, zeros past n.
-__device__ __forceinline__ void load8(const void *p, bool bf16, int at, int n, float *out) {
+// A warp's 256 elements of a tensor that may be of either type and start anywhere,
+// as bits: in w[0..7] a lane's eight consecutive ones, bf16 packed in pairs
+// into w[0..3].  Full warps of aligned tensors are read 16 (bf16) or 32 bytes (fp32) a
+// lane; the others element by element, lanes side by side, and turned in shared
+// memory (stage: 256 words of the warp's own), zeros past n.
+__device__ __forceinline__ void load_raw(const void *p, bool bf16, bool whole, int at, int n, uint32_t *stage, uint32_t *w) {
+    const int lane = threadIdx.x & 31;
+    if (whole) {
+        if (bf16) {
+            const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + at));
+            w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+        } else {
+            load_words8(static_cast<const float *>(p) + at, w);
+        }
+        return;
+    }
+    const int first = at - 8 * lane;
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        out[i] = 0.0f;
-        if (at + i < n)
-            out[i] = bf16 ? bf16_to_float(static_cast<const uint16_t *>(p)[at + i]) : static_cast<const float *>(p)[at + i];
+        const int k = first + 32 * i + lane;
+        uint32_t bits = 0;
+        if (k < n) bits = bf16 ? __ldcs(static_cast<const uint16_t *>(p) + k) : __ldcs(static_cast<const uint32_t *>(p) + k);
+        stage[32 * i + lane] = bits;
+    }
+    __syncwarp();
+    const uint4 a = reinterpret_cast<const uint4 *>(stage)[2 * lane], b = reinterpret_cast<const uint4 *>(stage)[2 * lane + 1];
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    if (bf16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = w[2 * i] | w[2 * i + 1] << 16;
+    }
+}
+__device__ __forceinline__ void store_raw(void *p, bool bf16, bool whole, int at, int n, uint32_t *stage, const uint32_t *w) {
+    const int lane = threadIdx.x & 31;
+    if (whole) {
+        if (bf16)
+            __stcs(reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + at), make_uint4(w[0], w[1], w[2], w[3]));
+        else
+            store_words8(static_cast<float *>(p) + at, w);
+        return;
+    }
+    const int first = at - 8 * lane;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) stage[8 * lane + i] = bf16 ? (w[i / 2] >> (16 * (i & 1))) & 0xffffu : w[i];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = first + 32 * i + lane;
+        if (k >= n) break;
+        if (bf16)
+            static_cast<uint16_t *>(p)[k] = static_cast<uint16_t>(stage[32 * i + lane]);
+        else
+            static_cast<uint32_t *>(p)[k] = stage[32 * i + lane];
+    }
+}
+__device__ __forceinline__ void to_floats(const uint32_t *w, bool bf16, float *x) {
+    if (bf16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
     }
 }
 
-// bf16 bits of x with a random 16-bit word added below them; a NaN stays one.
-__device__ __forceinline__ uint16_t bf16_random(float x, uint32_t word) {
+// Two values to bf16 bits, packed, each with a random 16-bit word added below them (a NaN stays
+// one); and to nearest.
+__device__ __forceinline__ uint32_t bf16_random(float x, uint32_t word) {
     const uint32_t bits = __float_as_uint(x);
-    return static_cast<uint16_t>((x != x ? bits | 0x400000u : bits + (word & 0xffffu)) >> 16);
+    return x != x ? bits | 0x400000u : bits + (word & 0xffffu);
 }
-__device__ __forceinline__ uint16_t bf16_nearest(float x) {
-    const uint32_t bits = __float_as_uint(x);
-    return static_cast<uint16_t>((x != x ? bits | 0x400000u : bits + 0x7fffu + ((bits >> 16) & 1u)) >> 16);
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __byte_perm(lo, hi, 0x7632); }
+__device__ __forceinline__ uint32_t bf16_nearest2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
 __device__ __forceinline__ float sqrt_approx(float x) {
@@ -61,9 +139,10 @@ __device__ __forceinline__ float ema(float b, float c, float s, float target) {
     return isinf(s) && c < 1.0f ? fmaf(c, target, s) : fmaf(c, target, fmaf(-c, s, s));
 }
 
-template <int BITS>
+template <int BITS, bool CLIP>
 __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
                                                                    const float *clip_scale) {
+    __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
     const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp * kAdamwBlock >= c.n) return;
@@ -71,23 +150,38 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
     const uint32_t block = c.block + warp;
     const int64_t e = static_cast<int64_t>(block) * kAdamwBlock + 8 * lane;
     const uint32_t replica = static_cast<uint32_t>(blockIdx.x / a.n_chunks);
-    const bool p16 = (c.flags & kAdamwParamBf16) != 0;
+    const bool p16 = (c.flags & kAdamwParamBf16) != 0, g16 = (c.flags & kAdamwGradBf16) != 0;
+    const bool full = (warp + 1) * kAdamwBlock <= c.n;
+    const bool p_whole = full && (c.flags & kAdamwParamAligned), g_whole = full && (c.flags & kAdamwGradAligned);
 
-    float g[8], p[8], m[8], v[8];
-    load8(c.g, (c.flags & kAdamwGradBf16) != 0, at, c.n, g);
-    load8(c.p, p16, at, c.n, p);
+    // every load before any arithmetic
+    uint32_t gw[8], pw[8];
+    float m[8], v[8];
+    uint2 cm, cv;
+    float scale_m, scale_v;
+    load_raw(c.g, g16, g_whole, at, c.n, stages[warp], gw);
+    load_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
     if constexpr (BITS == 8) {
-        decode_m(reinterpret_cast<const uint2 *>(a.m)[e / 8], a.m_scale[block], m);
-        decode_v(reinterpret_cast<const uint2 *>(a.v)[e / 8], a.v_scale[block], v);
+        cm = __ldcs(reinterpret_cast<const uint2 *>(a.m) + e / 8);
+        cv = __ldcs(reinterpret_cast<const uint2 *>(a.v) + e / 8);
+        scale_m = __ldcs(a.m_scale + block);
+        scale_v = __ldcs(a.v_scale + block);
     } else {
-        load8(static_cast<const float *>(a.m) + e, false, 0, 8, m);
-        load8(static_cast<const float *>(a.v) + e, false, 0, 8, v);
+        load_f32x8(static_cast<const float *>(a.m) + e, m);
+        load_f32x8(static_cast<const float *>(a.v) + e, v);
     }
-    const float s = clip_scale ? clip_scale[replica] : 1.0f;
+    const float s = CLIP ? clip_scale[replica] : 1.0f;
     const float keep = fmaf(-sc.decay, c.decay, 1.0f);
+    float g[8], p[8];
+    to_floats(gw, g16, g);
+    to_floats(pw, p16, p);
+    if constexpr (BITS == 8) {
+        decode_m(cm, scale_m, m);
+        decode_v(cv, scale_v, v);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float gi = __fmul_rn(g[i], s);
+        const float gi = CLIP ? __fmul_rn(g[i], s) : g[i];
         m[i] = ema<BITS>(sc.b1, sc.c1, m[i], gi);
         v[i] = ema<BITS>(sc.b2, sc.c2, v[i], __fmul_rn(gi, gi));
         p[i] = fmaf(-sc.step, __fdividef(m[i], fmaf(sqrt_approx(v[i]), sc.root, sc.eps)), p[i] * keep);
@@ -100,28 +194,28 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
         low = static_cast<uint32_t>(z);
         high = static_cast<uint32_t>(z >> 32);
     }
-    if constexpr (BITS == 8) {
-        float scale;
-        const uint2 cm = encode_m<true>(m, low, scale);
-        reinterpret_cast<uint2 *>(a.m)[e / 8] = cm;
-        if (lane == 0) a.m_scale[block] = scale;
-        const uint2 cv = encode_v<true>(v, high, scale);
-        reinterpret_cast<uint2 *>(a.v)[e / 8] = cv;
-        if (lane == 0) a.v_scale[block] = scale;
+    if (p16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            pw[i] = upper_halves(bf16_random(p[2 * i], low * place_odd(2 * i)),
+                                 bf16_random(p[2 * i + 1], low * place_odd(2 * i + 1)));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            static_cast<float *>(a.m)[e + i] = m[i];
-            static_cast<float *>(a.v)[e + i] = v[i];
-        }
+        for (int i = 0; i < 8; ++i) pw[i] = __float_as_uint(p[i]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (at + i >= c.n) break;
-        if (p16)
-            static_cast<uint16_t *>(c.p)[at + i] = bf16_random(p[i], low * place_odd(i));
-        else
-            static_cast<float *>(c.p)[at + i] = p[i];
+    store_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
+    if constexpr (BITS == 8) {
+        cm = encode_m<true>(m, low, scale_m);
+        __stcs(reinterpret_cast<uint2 *>(a.m) + e / 8, cm);
+        cv = encode_v<true>(v, high, scale_v);
+        __stcs(reinterpret_cast<uint2 *>(a.v) + e / 8, cv);
+        if (lane == 0) {
+            a.m_scale[block] = scale_m;
+            a.v_scale[block] = scale_v;
+        }
+    } else {
+        store_f32x8(static_cast<float *>(a.m) + e, m);
+        store_f32x8(static_cast<float *>(a.v) + e, v);
     }
 }
 
@@ -130,12 +224,18 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
 __global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const AdamwList a, double *partial) {
     const int replica = blockIdx.y;
     const AdamwChunk *chunks = a.chunks + replica * a.n_chunks;
+    __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
+    const int warp = threadIdx.x >> 5;
     Kahan sum;
     double wide = 0.0;
     for (int64_t k = blockIdx.x; k < a.n_chunks; k += gridDim.x) {
         const AdamwChunk c = load_chunk(chunks + k);
+        const bool g16 = (c.flags & kAdamwGradBf16) != 0;
+        const bool whole = (warp + 1) * kAdamwBlock <= c.n && (c.flags & kAdamwGradAligned);
+        uint32_t gw[8];
+        load_raw(c.g, g16, whole, 8 * threadIdx.x, c.n, stages[warp], gw);
         float g[8];
-        load8(c.g, (c.flags & kAdamwGradBf16) != 0, 8 * threadIdx.x, c.n, g);
+        to_floats(gw, g16, g);
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) q = fmaf(g[i], g[i], q);
@@ -206,6 +306,7 @@ __device__ __forceinline__ void mean8(int M, Get get, float *out) {
 
 template <int BITS>
 __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const AdamwList a, uint32_t mask) {
+    __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
     const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp * kAdamwBlock >= c.n) return;
@@ -213,21 +314,25 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
     const int64_t blocks = a.n_state / kAdamwBlock;
     const int64_t block = c.block + warp;
     const int64_t e = block * kAdamwBlock + 8 * lane;
+    const bool full = (warp + 1) * kAdamwBlock <= c.n;
     float mean[8];
     if (mask & 1u) {
         const bool p16 = (c.flags & kAdamwParamBf16) != 0;
-        mean8(a.M, [&](int r, float *s) { load8(load_chunk(a.chunks + r * a.n_chunks + blockIdx.x).p, p16, at, c.n, s); },
-              mean);
-        for (int r = 0; r < a.M; ++r) {
-            void *p = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x).p;
+        uint32_t w[8];
+        mean8(a.M, [&](int r, float *s) {
+            const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
+            load_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stages[warp], w);
+            to_floats(w, p16, s);
+        }, mean);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (at + i >= c.n) break;
-                if (p16)
-                    static_cast<uint16_t *>(p)[at + i] = bf16_nearest(mean[i]);
-                else
-                    static_cast<float *>(p)[at + i] = mean[i];
-            }
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(mean[i]);
+        if (p16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = bf16_nearest2(mean[2 * i], mean[2 * i + 1]);
+        }
+        for (int r = 0; r < a.M; ++r) {
+            const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
+            store_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stages[warp], w);
         }
     }
 #pragma unroll
@@ -237,22 +342,20 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
         float *scales = q == 0 ? a.m_scale : a.v_scale;
         if constexpr (BITS == 8) {
             mean8(a.M, [&](int r, float *s) {
-                const uint2 codes = static_cast<const uint2 *>(held)[(r * a.n_state + e) / 8];
-                const float scale = scales[r * blocks + block];
+                const uint2 codes = __ldcs(static_cast<const uint2 *>(held) + (r * a.n_state + e) / 8);
+                const float scale = __ldcs(scales + r * blocks + block);
                 if (q == 0) decode_m(codes, scale, s); else decode_v(codes, scale, s);
             }, mean);
             float scale;
             const uint2 codes = q == 0 ? encode_m<false>(mean, 0, scale) : encode_v<false>(mean, 0, scale);
             for (int r = 0; r < a.M; ++r) {
-                static_cast<uint2 *>(held)[(r * a.n_state + e) / 8] = codes;
+                __stcs(static_cast<uint2 *>(held) + (r * a.n_state + e) / 8, codes);
                 if (lane == 0) scales[r * blocks + block] = scale;
             }
         } else {
             float *s32 = static_cast<float *>(held);
-            mean8(a.M, [&](int r, float *s) { load8(s32 + r * a.n_state + e, false, 0, 8, s); }, mean);
-            for (int r = 0; r < a.M; ++r)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s32[r * a.n_state + e + i] = mean[i];
+            mean8(a.M, [&](int r, float *s) { load_f32x8(s32 + r * a.n_state + e, s); }, mean);
+            for (int r = 0; r < a.M; ++r) store_f32x8(s32 + r * a.n_state + e, mean);
         }
     }
 }
@@ -275,16 +378,19 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_bind_kernel(AdamwChunk *c
     const bool bf16 = dtype[lo] == MTDAO_BF16;
     AdamwChunk &c = chunks[blockIdx.y * n_chunks + k];
     char *p = static_cast<char *>(table[static_cast<int64_t>(blockIdx.y) * n_tensors + lo]) + first * (bf16 ? 2 : 4);
+    const bool aligned = reinterpret_cast<uintptr_t>(p) % (bf16 ? 16 : 32) == 0;
     if (grads) {
         c.g = p;
-        c.flags = (c.flags & ~kAdamwGradBf16) | (bf16 ? kAdamwGradBf16 : 0u);
+        c.flags = (c.flags & ~(kAdamwGradBf16 | kAdamwGradAligned)) | (bf16 ? kAdamwGradBf16 : 0u) |
+                  (aligned ? kAdamwGradAligned : 0u);
         return;
     }
     const int64_t left = t.numel - first;
     c.p = p;
     c.block = static_cast<uint32_t>(blockIdx.y * n_blocks + t.first_block + first / kAdamwBlock);
     c.n = static_cast<int32_t>(left < kAdamwChunk ? left : kAdamwChunk);
-    c.flags = (c.flags & ~kAdamwParamBf16) | (bf16 ? kAdamwParamBf16 : 0u);
+    c.flags = (c.flags & ~(kAdamwParamBf16 | kAdamwParamAligned)) | (bf16 ? kAdamwParamBf16 : 0u) |
+              (aligned ? kAdamwParamAligned : 0u);
     c.decay = t.decay;
 }
 
@@ -301,10 +407,9 @@ cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, in
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {
     const unsigned grid = static_cast<unsigned>(a.n_chunks * a.M);
-    if (a.bits == 8)
-        adamw_step_kernel<8><<<grid, kAdamwThreads, 0, stream>>>(a, sc, clip_scale);
-    else
-        adamw_step_kernel<32><<<grid, kAdamwThreads, 0, stream>>>(a, sc, clip_scale);
+    auto kernel = a.bits == 8 ? (clip_scale ? adamw_step_kernel<8, true> : adamw_step_kernel<8, false>)
+                              : (clip_scale ? adamw_step_kernel<32, true> : adamw_step_kernel<32, false>);
+    kernel<<<grid, kAdamwThreads, 0, stream>>>(a, sc, clip_scale);
     return cudaGetLastError();
 }
 

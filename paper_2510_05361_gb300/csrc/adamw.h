@@ -24,6 +24,8 @@ struct __align__(16) AdamwChunk {
     float decay;              // the tensor's decay factor
 };
 constexpr uint32_t kAdamwParamBf16 = 1, kAdamwGradBf16 = 2;
+// eight elements start at a multiple of their size: one access of a lane
+constexpr uint32_t kAdamwParamAligned = 4, kAdamwGradAligned = 8;
 
 // What does not depend on the step.
 struct AdamwList {

@@ -25,6 +25,7 @@ struct mtdao_adamw_ctx {
     int32_t n_tensors = 0;
     std::vector<AdamwTensor> tensors;
     AdamwList list = {};
+    void *memory = nullptr;              // the one allocation; what follows lies in it
     AdamwChunk *chunks = nullptr;
     AdamwTensor *tensors_dev = nullptr;
     void **table = nullptr;              // [M][n_tensors], scratch of a binding
@@ -73,10 +74,7 @@ int select_device(mtdao_adamw_ctx *h) {
 
 void release(mtdao_adamw_ctx *h) {
     cudaStreamSynchronize(h->stream);
-    void *owned[] = {h->list.m, h->list.v, h->list.m_scale, h->list.v_scale, h->chunks, h->tensors_dev,
-                     h->table, h->dtypes, h->norm_partial, h->norm_sums, h->clip_scale};
-    for (void *p : owned)
-        if (p) cudaFree(p);
+    if (h->memory) cudaFree(h->memory);
 }
 
 bool rate(double b) { return b >= 0.0 && b < 1.0; }
@@ -120,38 +118,36 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
     struct {
         void **p;
         size_t bytes;
-        const char *what;
     } allocs[] = {
-        {&a.m, held, "m"},
-        {&a.v, held, "v"},
-        {reinterpret_cast<void **>(&a.m_scale), scales, "m's scales"},
-        {reinterpret_cast<void **>(&a.v_scale), scales, "v's scales"},
-        {reinterpret_cast<void **>(&h->chunks), static_cast<size_t>(M) * chunks * sizeof(AdamwChunk), "records"},
-        {reinterpret_cast<void **>(&h->tensors_dev), n_tensors * sizeof(AdamwTensor), "tensor list"},
-        {reinterpret_cast<void **>(&h->table), static_cast<size_t>(M) * n_tensors * sizeof(void *), "address table"},
-        {reinterpret_cast<void **>(&h->dtypes), n_tensors * sizeof(int32_t), "type table"},
-        {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(M) * h->norm_blocks * sizeof(double),
-         "norm partials"},
-        {reinterpret_cast<void **>(&h->norm_sums), M * sizeof(double), "norms"},
-        {reinterpret_cast<void **>(&h->clip_scale), M * sizeof(float), "clip factors"},
+        {&a.m, held},
+        {&a.v, held},
+        {reinterpret_cast<void **>(&a.m_scale), scales},
+        {reinterpret_cast<void **>(&a.v_scale), scales},
+        {reinterpret_cast<void **>(&h->chunks), static_cast<size_t>(M) * chunks * sizeof(AdamwChunk)},
+        {reinterpret_cast<void **>(&h->tensors_dev), n_tensors * sizeof(AdamwTensor)},
+        {reinterpret_cast<void **>(&h->table), static_cast<size_t>(M) * n_tensors * sizeof(void *)},
+        {reinterpret_cast<void **>(&h->dtypes), n_tensors * sizeof(int32_t)},
+        {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(M) * h->norm_blocks * sizeof(double)},
+        {reinterpret_cast<void **>(&h->norm_sums), M * sizeof(double)},
+        {reinterpret_cast<void **>(&h->clip_scale), M * sizeof(float)},
     };
+    // one allocation: a call to the driver costs more than setting up a small list
+    size_t total = 0;
+    for (auto &x : allocs) total += (x.bytes + 255) / 256 * 256;
+    e = cudaMalloc(&h->memory, total);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        h->memory = nullptr;
+        return fail(nullptr, MTDAO_ERR_OOM, "cudaMalloc of states and tables (%zu bytes) failed: %s", total,
+                    cudaGetErrorString(e));
+    }
+    size_t at = 0;
     for (auto &x : allocs) {
-        if (x.bytes == 0) continue;
-        e = cudaMalloc(x.p, x.bytes);
-        if (e != cudaSuccess) {
-            cudaGetLastError();
-            *x.p = nullptr;
-            return fail(nullptr, MTDAO_ERR_OOM, "cudaMalloc of %s (%zu bytes) failed: %s", x.what, x.bytes,
-                        cudaGetErrorString(e));
-        }
+        if (x.bytes) *x.p = static_cast<char *>(h->memory) + at;
+        at += (x.bytes + 255) / 256 * 256;
     }
     a.chunks = h->chunks;
-    e = cudaMemsetAsync(a.m, 0, held, h->stream);
-    if (e == cudaSuccess) e = cudaMemsetAsync(a.v, 0, held, h->stream);
-    if (e == cudaSuccess && scales) e = cudaMemsetAsync(a.m_scale, 0, scales, h->stream);
-    if (e == cudaSuccess && scales) e = cudaMemsetAsync(a.v_scale, 0, scales, h->stream);
-    if (e == cudaSuccess)
-        e = cudaMemsetAsync(h->chunks, 0, static_cast<size_t>(M) * chunks * sizeof(AdamwChunk), h->stream);
+    e = cudaMemsetAsync(h->memory, 0, total, h->stream);
     if (e == cudaSuccess)
         e = cudaMemcpyAsync(h->tensors_dev, h->tensors.data(), n_tensors * sizeof(AdamwTensor), cudaMemcpyHostToDevice,
                             h->stream);
