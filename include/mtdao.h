@@ -493,7 +493,7 @@ const char *mtdao_last_error(mtdao_handle h);
  *   m  = beta1 m + (1 - beta1) g'          v = beta2 v + (1 - beta2) g'^2
  *   p  = p (1 - lr weight_decay decay_k)
  *        - lr (m / (1 - beta1^(t+1))) / (sqrt(v / (1 - beta2^(t+1))) + eps)
- * computed in fp32 (square root and quotient to 2 units in the last place).
+ * computed in fp32 (square root and quotient to 2^-22 of their value).
  *
  * State vectors: tensor k starts at a multiple of MTDAO_ADAMW_BLOCK elements
  * (numels rounded up), so that a block of that many elements belongs to one
@@ -520,7 +520,7 @@ const char *mtdao_last_error(mtdao_handle h);
 
 typedef struct {
     double beta1, beta2;                /* in [0, 1) */
-    double eps;                         /* 1e-30 <= eps */
+    double eps;                         /* >= 1e-15: v below 2^-126 counts as zero in the update */
     int32_t state_bits;                 /* 32 or 8 */
     uint64_t seed;                      /* of the stochastic rounding */
 } mtdao_adamw_config;

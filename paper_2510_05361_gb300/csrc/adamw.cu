@@ -115,7 +115,7 @@ __device__ __forceinline__ void to_floats(const uint32_t *w, bool bf16, float *x
 // one); and to nearest.
 __device__ __forceinline__ uint32_t bf16_random(float x, uint32_t word) {
     const uint32_t bits = __float_as_uint(x);
-    return x != x ? bits | 0x400000u : bits + (word & 0xffffu);
+    return x != x ? 0x7fffffffu : bits + (word & 0xffffu);
 }
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __byte_perm(lo, hi, 0x7632); }
 __device__ __forceinline__ uint32_t bf16_nearest2(float lo, float hi) {
@@ -126,30 +126,36 @@ __device__ __forceinline__ uint32_t bf16_nearest2(float lo, float hi) {
 
 __device__ __forceinline__ float sqrt_approx(float x) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
-// m and v are formed with a rounding after each operation in 8 bits: what the
-// formula gives then does not depend on the compiler's choice of fused operations.
-// In 32 bits the products stay unrounded (one rounding less for each).
-template <int BITS>
-__device__ __forceinline__ float ema(float b, float c, float s, float target) {
-    if constexpr (BITS == 8) return __fadd_rn(__fmul_rn(s, b), __fmul_rn(target, c));
+// m and v in 32 bits: the products stay unrounded; an infinity stays one.
+__device__ __forceinline__ float ema(float c, float s, float target) {
     return isinf(s) && c < 1.0f ? fmaf(c, target, s) : fmaf(c, target, fmaf(-c, s, s));
 }
 
+// One block of 256 elements a warp.  In 8 bits m and v are formed with a rounding
+// after each operation: what the formula gives then does not depend on a compiler's
+// choice of fused operations, and a test can ask for its very codes.  beta multiplies the
+// block's scale, a power of two, rather than each value.  The square root and the
+// reciprocal are the hardware's (2^-22): their error is far below an update's effect on p.
 template <int BITS, bool CLIP>
 __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
                                                                    const float *clip_scale) {
     __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
-    const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);
+    const uint32_t replica = blockIdx.y;
+    const AdamwChunk c = load_chunk(a.chunks + replica * a.n_chunks + blockIdx.x);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (warp * kAdamwBlock >= c.n) return;
     const int at = warp * kAdamwBlock + 8 * lane;
     const uint32_t block = c.block + warp;
-    const int64_t e = static_cast<int64_t>(block) * kAdamwBlock + 8 * lane;
-    const uint32_t replica = static_cast<uint32_t>(blockIdx.x / a.n_chunks);
+    const int64_t eight = static_cast<int64_t>(block) * (kAdamwBlock / 8) + lane;   // the lane's, in groups of eight
     const bool p16 = (c.flags & kAdamwParamBf16) != 0, g16 = (c.flags & kAdamwGradBf16) != 0;
     const bool full = (warp + 1) * kAdamwBlock <= c.n;
     const bool p_whole = full && (c.flags & kAdamwParamAligned), g_whole = full && (c.flags & kAdamwGradAligned);
@@ -159,38 +165,43 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
     float m[8], v[8];
     uint2 cm, cv;
     float scale_m, scale_v;
-    load_raw(c.g, g16, g_whole, at, c.n, stages[warp], gw);
-    load_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
     if constexpr (BITS == 8) {
-        cm = __ldcs(reinterpret_cast<const uint2 *>(a.m) + e / 8);
-        cv = __ldcs(reinterpret_cast<const uint2 *>(a.v) + e / 8);
+        cm = __ldcs(static_cast<const uint2 *>(a.m) + eight);
+        cv = __ldcs(static_cast<const uint2 *>(a.v) + eight);
         scale_m = __ldcs(a.m_scale + block);
         scale_v = __ldcs(a.v_scale + block);
     } else {
-        load_f32x8(static_cast<const float *>(a.m) + e, m);
-        load_f32x8(static_cast<const float *>(a.v) + e, v);
+        load_f32x8(static_cast<const float *>(a.m) + 8 * eight, m);
+        load_f32x8(static_cast<const float *>(a.v) + 8 * eight, v);
     }
+    load_raw(c.g, g16, g_whole, at, c.n, stages[warp], gw);
+    load_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
     const float s = CLIP ? clip_scale[replica] : 1.0f;
     const float keep = fmaf(-sc.decay, c.decay, 1.0f);
     float g[8], p[8];
     to_floats(gw, g16, g);
     to_floats(pw, p16, p);
     if constexpr (BITS == 8) {
-        decode_m(cm, scale_m, m);
-        decode_v(cv, scale_v, v);
+        decode_m(cm, sc.b1 * scale_m, m);
+        decode_v(cv, sc.b2 * scale_v, v);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float gi = CLIP ? __fmul_rn(g[i], s) : g[i];
-        m[i] = ema<BITS>(sc.b1, sc.c1, m[i], gi);
-        v[i] = ema<BITS>(sc.b2, sc.c2, v[i], __fmul_rn(gi, gi));
-        p[i] = fmaf(-sc.step, __fdividef(m[i], fmaf(sqrt_approx(v[i]), sc.root, sc.eps)), p[i] * keep);
+        if constexpr (BITS == 8) {
+            m[i] = __fadd_rn(m[i], __fmul_rn(gi, sc.c1));
+            v[i] = __fadd_rn(v[i], __fmul_rn(__fmul_rn(gi, gi), sc.c2));
+        } else {
+            m[i] = ema(sc.c1, m[i], gi);
+            v[i] = ema(sc.c2, v[i], __fmul_rn(gi, gi));
+        }
+        p[i] = fmaf(-sc.step * m[i], rcp_approx(fmaf(sqrt_approx(v[i]), sc.root, sc.eps)), p[i] * keep);
     }
     uint32_t low = 0, high = 0;
     if (BITS == 8 || p16) {
-        const uint64_t blocks = static_cast<uint64_t>(a.n_state) / kAdamwBlock;
-        const uint64_t group = (block - replica * blocks) * (kAdamwBlock / 8) + lane;
-        const uint64_t z = splitmix64(sc.key + ((static_cast<uint64_t>(replica) << 32) + group) * kGolden);
+        const uint32_t first = block - replica * static_cast<uint32_t>(a.n_state / kAdamwBlock);
+        const uint64_t counter = (static_cast<uint64_t>(replica) << 32) + first * (kAdamwBlock / 8) + lane;
+        const uint64_t z = splitmix64(sc.key + counter * kGolden);
         low = static_cast<uint32_t>(z);
         high = static_cast<uint32_t>(z >> 32);
     }
@@ -206,16 +217,16 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
     store_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
     if constexpr (BITS == 8) {
         cm = encode_m<true>(m, low, scale_m);
-        __stcs(reinterpret_cast<uint2 *>(a.m) + e / 8, cm);
+        __stcs(static_cast<uint2 *>(a.m) + eight, cm);
         cv = encode_v<true>(v, high, scale_v);
-        __stcs(reinterpret_cast<uint2 *>(a.v) + e / 8, cv);
+        __stcs(static_cast<uint2 *>(a.v) + eight, cv);
         if (lane == 0) {
             a.m_scale[block] = scale_m;
             a.v_scale[block] = scale_v;
         }
     } else {
-        store_f32x8(static_cast<float *>(a.m) + e, m);
-        store_f32x8(static_cast<float *>(a.v) + e, v);
+        store_f32x8(static_cast<float *>(a.m) + 8 * eight, m);
+        store_f32x8(static_cast<float *>(a.v) + 8 * eight, v);
     }
 }
 
@@ -406,7 +417,7 @@ cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, in
 }
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {
-    const unsigned grid = static_cast<unsigned>(a.n_chunks * a.M);
+    const dim3 grid(static_cast<unsigned>(a.n_chunks), a.M);
     auto kernel = a.bits == 8 ? (clip_scale ? adamw_step_kernel<8, true> : adamw_step_kernel<8, false>)
                               : (clip_scale ? adamw_step_kernel<32, true> : adamw_step_kernel<32, false>);
     kernel<<<grid, kAdamwThreads, 0, stream>>>(a, sc, clip_scale);

@@ -97,8 +97,8 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
         if (blocks > 0xffffffffll) break;
     }
     if (blocks == 0) return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list holds no element");
-    // the records count blocks in 32 bits, the launches chunks in 31, the random numbers groups of 8 in 32
-    if (blocks * M > 0xffffffffll || chunks * M > 0x7fffffffll || blocks * (kAdamwBlock / 8) > 0xffffffffll)
+    // the records count blocks in 32 bits, a grid a replica's chunks in 31, the random numbers groups of 8 in 32
+    if (blocks * M > 0xffffffffll || chunks > 0x7fffffffll || blocks * (kAdamwBlock / 8) > 0xffffffffll)
         return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list is too long for %d replicas", M);
 
     h->stream = static_cast<cudaStream_t>(cuda_stream);
@@ -198,8 +198,8 @@ extern "C" int mtdao_adamw_create(const mtdao_adamw_config *cfg, int32_t M, cons
     if (cfg == nullptr) return set_thread_error(MTDAO_ERR_INVALID, "config is NULL");
     if (!rate(cfg->beta1) || !rate(cfg->beta2))
         return fail(nullptr, MTDAO_ERR_INVALID, "beta1=%g, beta2=%g must lie in [0,1)", cfg->beta1, cfg->beta2);
-    if (!(std::isfinite(cfg->eps) && cfg->eps >= 1e-30))
-        return fail(nullptr, MTDAO_ERR_INVALID, "eps=%g must be at least 1e-30", cfg->eps);
+    if (!(std::isfinite(cfg->eps) && cfg->eps >= 1e-15))
+        return fail(nullptr, MTDAO_ERR_INVALID, "eps=%g must be at least 1e-15", cfg->eps);
     if (cfg->state_bits != 8 && cfg->state_bits != 32)
         return fail(nullptr, MTDAO_ERR_INVALID, "state_bits=%d must be 8 or 32", cfg->state_bits);
     if (M < 1 || M > MTDAO_MAX_REPLICAS)

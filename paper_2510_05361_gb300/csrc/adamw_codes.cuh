@@ -33,15 +33,28 @@ struct CodeV {
     static constexpr int kTop = 14, kDrop = 21;
 };
 
-// The scale of a block whose largest magnitude is given as fp32 bits, and its
-// inverse: powers of two, so that scaling rounds nothing.
+// The scale of a block of a given largest magnitude, and its inverse: powers of two, so that
+// scaling rounds nothing.
 template <typename Code>
-__device__ __forceinline__ void block_scale(uint32_t largest, float &scale, float &inverse) {
-    const uint32_t e = largest >> 23;
+__device__ __forceinline__ void block_scale(float largest, float &scale, float &inverse) {
+    const uint32_t e = __float_as_uint(largest) >> 23;
     scale = __uint_as_float((e - Code::kTop) << 23);
     inverse = __uint_as_float((254u - e + Code::kTop) << 23);
-    if (largest < (17u << 23)) scale = inverse = 0.0f;                        // below 2^-110
-    if (e == 255u) scale = inverse = __uint_as_float(0x7fffffffu);            // an infinity or a NaN
+    if (e < 17u) scale = inverse = 0.0f;                                      // below 2^-110
+    if (e >= 255u) scale = inverse = __uint_as_float(0x7fffffffu);            // an infinity or a NaN
+}
+
+// The largest magnitude of eight values of every lane of the warp; a NaN where there is one.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float block_max(const float *x) {
+    const float lane = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], 0.0f));
+    float r;
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(lane));
+    return r;
 }
 
 // y, moved within half a code step either way by the given random word: the nearest code of
@@ -74,11 +87,11 @@ __device__ __forceinline__ float2 unpack_e4m3(uint32_t two) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
     return half2_to_float2(h);
 }
-__device__ __forceinline__ float2 unpack_e5m2(uint32_t two) {
-    return half2_to_float2(((two & 0xffu) << 8) | ((two & 0xff00u) << 16));     // e5m2 is fp16's upper half
+__device__ __forceinline__ float2 unpack_e5m2(uint32_t four, int upper) {        // e5m2 is fp16's upper half
+    return half2_to_float2(__byte_perm(four, 0u, upper ? 0x3424 : 0x1404));
 }
 
-// Eight codes of a lane to values, and back.
+// Eight codes of a lane to values: the codes times scale.
 __device__ __forceinline__ void decode_m(uint2 c, float scale, float *m) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -90,7 +103,7 @@ __device__ __forceinline__ void decode_m(uint2 c, float scale, float *m) {
 __device__ __forceinline__ void decode_v(uint2 c, float scale, float *v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 t = unpack_e5m2((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
+        const float2 t = unpack_e5m2((i < 2 ? c.x : c.y), i & 1);
         v[2 * i] = t.x * scale;
         v[2 * i + 1] = t.y * scale;
     }
@@ -100,34 +113,26 @@ __device__ __forceinline__ void decode_v(uint2 c, float scale, float *v) {
 // random word times each place's constant, else to nearest.  The whole warp calls it.
 template <bool RANDOM>
 __device__ __forceinline__ uint2 encode_m(const float *m, uint32_t word, float &scale) {
-    uint32_t largest = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) largest = max(largest, __float_as_uint(m[i]) & 0x7fffffffu);
-    float inverse;
-    block_scale<CodeM>(__reduce_max_sync(0xffffffffu, largest), scale, inverse);
-    float y[8];
+    float inverse, y[8];
+    block_scale<CodeM>(block_max(m), scale, inverse);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         y[i] = m[i] * inverse;
         // what is too small to count must not meet the move: it would borrow from the sign
-        if constexpr (RANDOM) y[i] = fabsf(y[i]) < 0x1p-30f ? 0.0f : moved<CodeM>(y[i], word * place_odd(i));
+        if (RANDOM && fabsf(y[i]) >= 0x1p-30f) y[i] = moved<CodeM>(y[i], word * place_odd(i));
     }
     return make_uint2(pack_e4m3(y[0], y[1]) | pack_e4m3(y[2], y[3]) << 16,
                       pack_e4m3(y[4], y[5]) | pack_e4m3(y[6], y[7]) << 16);
 }
 template <bool RANDOM>
 __device__ __forceinline__ uint2 encode_v(const float *v, uint32_t word, float &scale) {
-    uint32_t largest = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) largest = max(largest, __float_as_uint(v[i]) & 0x7fffffffu);
-    float inverse;
-    block_scale<CodeV>(__reduce_max_sync(0xffffffffu, largest), scale, inverse);
+    float inverse, y[8];
+    block_scale<CodeV>(block_max(v), scale, inverse);
     if (inverse == 0.0f) return make_uint2(0u, 0u);
-    float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         y[i] = fmaxf(v[i] * inverse, 0x1p-16f);
-        if constexpr (RANDOM) y[i] = moved<CodeV>(y[i], word * place_odd(i));
+        if (RANDOM) y[i] = moved<CodeV>(y[i], word * place_odd(i));
     }
     return make_uint2(pack_e5m2(y[0], y[1]) | pack_e5m2(y[2], y[3]) << 16,
                       pack_e5m2(y[4], y[5]) | pack_e5m2(y[6], y[7]) << 16);
