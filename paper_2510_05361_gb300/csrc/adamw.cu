@@ -36,10 +36,6 @@ __device__ __forceinline__ void store_words8(void *p, const uint32_t *w) {
                  :: "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p)
                  : "memory");
 }
-__device__ __forceinline__ void load_f32x8(const float *p, float *x) { load_words8(p, reinterpret_cast<uint32_t *>(x)); }
-__device__ __forceinline__ void store_f32x8(float *p, const float *x) {
-    store_words8(p, reinterpret_cast<const uint32_t *>(x));
-}
 
 // A warp's 256 elements of a tensor that may be of either type and start anywhere,
 // as bits: in w[0..7] a lane's eight consecutive ones, bf16 packed in pairs
@@ -98,24 +94,32 @@ __device__ __forceinline__ void store_raw(void *p, bool bf16, bool whole, int at
             static_cast<uint32_t *>(p)[k] = stage[32 * i + lane];
     }
 }
-__device__ __forceinline__ void to_floats(const uint32_t *w, bool bf16, float *x) {
+__device__ __forceinline__ void to_pairs(const uint32_t *w, bool bf16, Pair *x) {
     if (bf16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) x[i] = Pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+        for (int i = 0; i < 4; ++i) x[i] = Pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
     }
+}
+__device__ __forceinline__ void load_pairs(const float *p, Pair *x) {
+    uint32_t w[8];
+    load_words8(p, w);
+    to_pairs(w, false, x);
+}
+__device__ __forceinline__ void store_pairs(float *p, const Pair *x) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(i & 1 ? x[i / 2].hi() : x[i / 2].lo());
+    store_words8(p, w);
 }
 
 // Two values to bf16 bits, packed, each with a random 16-bit word added below them (a NaN stays
 // one); and to nearest.
 __device__ __forceinline__ uint32_t bf16_random(float x, uint32_t word) {
     const uint32_t bits = __float_as_uint(x);
-    return x != x ? 0x7fffffffu : bits + (word & 0xffffu);
+    return x == x ? bits + (word & 0xffffu) : bits;      // arithmetic's NaN has every bit set below the sign
 }
 __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __byte_perm(lo, hi, 0x7632); }
 __device__ __forceinline__ uint32_t bf16_nearest2(float lo, float hi) {
@@ -146,7 +150,7 @@ __device__ __forceinline__ float ema(float c, float s, float target) {
 // block's scale, a power of two, rather than each value.  The square root and the
 // reciprocal are the hardware's (2^-22): their error is far below an update's effect on p.
 template <int BITS, bool CLIP>
-__global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
+__global__ void __launch_bounds__(kAdamwThreads, 5) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
                                                                    const float *clip_scale) {
     __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
     const uint32_t replica = blockIdx.y;
@@ -162,7 +166,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
 
     // every load before any arithmetic
     uint32_t gw[8], pw[8];
-    float m[8], v[8];
+    Pair m[4], v[4];
     uint2 cm, cv;
     float scale_m, scale_v;
     if constexpr (BITS == 8) {
@@ -171,31 +175,33 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
         scale_m = __ldcs(a.m_scale + block);
         scale_v = __ldcs(a.v_scale + block);
     } else {
-        load_f32x8(static_cast<const float *>(a.m) + 8 * eight, m);
-        load_f32x8(static_cast<const float *>(a.v) + 8 * eight, v);
+        load_pairs(static_cast<const float *>(a.m) + 8 * eight, m);
+        load_pairs(static_cast<const float *>(a.v) + 8 * eight, v);
     }
     load_raw(c.g, g16, g_whole, at, c.n, stages[warp], gw);
     load_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
     const float s = CLIP ? clip_scale[replica] : 1.0f;
     const float keep = fmaf(-sc.decay, c.decay, 1.0f);
-    float g[8], p[8];
-    to_floats(gw, g16, g);
-    to_floats(pw, p16, p);
+    Pair g[4], p[4];
+    to_pairs(gw, g16, g);
+    to_pairs(pw, p16, p);
     if constexpr (BITS == 8) {
         decode_m(cm, sc.b1 * scale_m, m);
         decode_v(cv, sc.b2 * scale_v, v);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float gi = CLIP ? __fmul_rn(g[i], s) : g[i];
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (CLIP) g[i] = product(g[i], Pair(s));
         if constexpr (BITS == 8) {
-            m[i] = __fadd_rn(m[i], __fmul_rn(gi, sc.c1));
-            v[i] = __fadd_rn(v[i], __fmul_rn(__fmul_rn(gi, gi), sc.c2));
+            m[i] = m[i] + product(g[i], Pair(sc.c1));
+            v[i] = v[i] + product(g[i] * g[i], Pair(sc.c2));
         } else {
-            m[i] = ema(sc.c1, m[i], gi);
-            v[i] = ema(sc.c2, v[i], __fmul_rn(gi, gi));
+            const Pair q = g[i] * g[i];
+            m[i] = Pair(ema(sc.c1, m[i].lo(), g[i].lo()), ema(sc.c1, m[i].hi(), g[i].hi()));
+            v[i] = Pair(ema(sc.c2, v[i].lo(), q.lo()), ema(sc.c2, v[i].hi(), q.hi()));
         }
-        p[i] = fmaf(-sc.step * m[i], rcp_approx(fmaf(sqrt_approx(v[i]), sc.root, sc.eps)), p[i] * keep);
+        const Pair d = fma2(Pair(sqrt_approx(v[i].lo()), sqrt_approx(v[i].hi())), Pair(sc.root), Pair(sc.eps));
+        p[i] = fma2(m[i] * Pair(-sc.step), Pair(rcp_approx(d.lo()), rcp_approx(d.hi())), p[i] * Pair(keep));
     }
     uint32_t low = 0, high = 0;
     if (BITS == 8 || p16) {
@@ -208,11 +214,11 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
     if (p16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            pw[i] = upper_halves(bf16_random(p[2 * i], low * place_odd(2 * i)),
-                                 bf16_random(p[2 * i + 1], low * place_odd(2 * i + 1)));
+            pw[i] = upper_halves(bf16_random(p[i].lo(), low * place_odd(2 * i)),
+                                 bf16_random(p[i].hi(), low * place_odd(2 * i + 1)));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pw[i] = __float_as_uint(p[i]);
+        for (int i = 0; i < 8; ++i) pw[i] = __float_as_uint(i & 1 ? p[i / 2].hi() : p[i / 2].lo());
     }
     store_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
     if constexpr (BITS == 8) {
@@ -225,8 +231,8 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_step_kernel(const AdamwLi
             a.v_scale[block] = scale_v;
         }
     } else {
-        store_f32x8(static_cast<float *>(a.m) + 8 * eight, m);
-        store_f32x8(static_cast<float *>(a.v) + 8 * eight, v);
+        store_pairs(static_cast<float *>(a.m) + 8 * eight, m);
+        store_pairs(static_cast<float *>(a.v) + 8 * eight, v);
     }
 }
 
@@ -245,11 +251,15 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const AdamwLi
         const bool whole = (warp + 1) * kAdamwBlock <= c.n && (c.flags & kAdamwGradAligned);
         uint32_t gw[8];
         load_raw(c.g, g16, whole, 8 * threadIdx.x, c.n, stages[warp], gw);
+        Pair gp[4], qp = Pair(0.0f);
+        to_pairs(gw, g16, gp);
         float g[8];
-        to_floats(gw, g16, g);
-        float q = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q = fmaf(g[i], g[i], q);
+        for (int i = 0; i < 4; ++i) {
+            qp = fma2(gp[i], gp[i], qp);
+            gp[i].get(g[2 * i], g[2 * i + 1]);
+        }
+        const float q = qp.lo() + qp.hi();
         if (q >= 0x1p-90f && q <= 0x1p100f) {
             sum.add(q);
         } else {                                     // zeros, or squares that fp32 does not hold
@@ -286,33 +296,37 @@ __global__ void __launch_bounds__(32) adamw_norm_last_kernel(const double *parti
 
 // The mean over the replicas of what get(r) gives; see replica_mean.cuh.
 template <typename Get>
-__device__ __forceinline__ void mean8(int M, Get get, float *out) {
-    float s[8];
+__device__ __forceinline__ void mean8(int M, Get get, Pair *out) {
+    Pair s[4];
     get(0, s);
     DiffSum sum[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = DiffSum(s[i]);
+    for (int i = 0; i < 8; ++i) sum[i] = DiffSum(i & 1 ? s[i / 2].hi() : s[i / 2].lo());
     for (int r = 1; r < M; ++r) {
         get(r, s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i].add(s[i]);
+        for (int i = 0; i < 8; ++i) sum[i].add(i & 1 ? s[i / 2].hi() : s[i / 2].lo());
     }
+    float mean[8];
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float q = sum[i].partial() / static_cast<float>(M);
-        out[i] = q == 0.0f ? sum[i].s0 : sum[i].s0 + q;
-        odd |= out[i] != out[i];
+        mean[i] = q == 0.0f ? sum[i].s0 : sum[i].s0 + q;
+        odd |= mean[i] != mean[i];
     }
-    if (!odd) return;
-    float plain[8] = {};
-    for (int r = 0; r < M; ++r) {
-        get(r, s);
+    if (__any_sync(0xffffffffu, odd)) {              // get() may need the whole warp
+        float plain[8] = {};
+        for (int r = 0; r < M; ++r) {
+            get(r, s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) plain[i] += s[i];
+            for (int i = 0; i < 8; ++i) plain[i] += i & 1 ? s[i / 2].hi() : s[i / 2].lo();
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mean[i] = mean_or_plain(mean[i], plain[i], static_cast<float>(M));
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = mean_or_plain(out[i], plain[i], static_cast<float>(M));
+    for (int i = 0; i < 4; ++i) out[i] = Pair(mean[2 * i], mean[2 * i + 1]);
 }
 
 template <int BITS>
@@ -326,20 +340,20 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
     const int64_t block = c.block + warp;
     const int64_t e = block * kAdamwBlock + 8 * lane;
     const bool full = (warp + 1) * kAdamwBlock <= c.n;
-    float mean[8];
+    Pair mean[4];
     if (mask & 1u) {
         const bool p16 = (c.flags & kAdamwParamBf16) != 0;
         uint32_t w[8];
-        mean8(a.M, [&](int r, float *s) {
+        mean8(a.M, [&](int r, Pair *s) {
             const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
             load_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stages[warp], w);
-            to_floats(w, p16, s);
+            to_pairs(w, p16, s);
         }, mean);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(mean[i]);
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(i & 1 ? mean[i / 2].hi() : mean[i / 2].lo());
         if (p16) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = bf16_nearest2(mean[2 * i], mean[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) w[i] = bf16_nearest2(mean[i].lo(), mean[i].hi());
         }
         for (int r = 0; r < a.M; ++r) {
             const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
@@ -352,7 +366,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
         void *held = q == 0 ? a.m : a.v;
         float *scales = q == 0 ? a.m_scale : a.v_scale;
         if constexpr (BITS == 8) {
-            mean8(a.M, [&](int r, float *s) {
+            mean8(a.M, [&](int r, Pair *s) {
                 const uint2 codes = __ldcs(static_cast<const uint2 *>(held) + (r * a.n_state + e) / 8);
                 const float scale = __ldcs(scales + r * blocks + block);
                 if (q == 0) decode_m(codes, scale, s); else decode_v(codes, scale, s);
@@ -365,8 +379,8 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
             }
         } else {
             float *s32 = static_cast<float *>(held);
-            mean8(a.M, [&](int r, float *s) { load_f32x8(s32 + r * a.n_state + e, s); }, mean);
-            for (int r = 0; r < a.M; ++r) store_f32x8(s32 + r * a.n_state + e, mean);
+            mean8(a.M, [&](int r, Pair *s) { load_pairs(s32 + r * a.n_state + e, s); }, mean);
+            for (int r = 0; r < a.M; ++r) store_pairs(s32 + r * a.n_state + e, mean);
         }
     }
 }

@@ -33,6 +33,38 @@ struct CodeV {
     static constexpr int kTop = 14, kDrop = 21;
 };
 
+// Two fp32 operations in one instruction, each rounded as the single ones are.
+struct Pair {
+    uint64_t bits;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit Pair(float both) : Pair(both, both) {}
+    __device__ __forceinline__ void get(float &lo, float &hi) const {
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(bits));
+    }
+    __device__ __forceinline__ float lo() const { float a, b; get(a, b); return a; }
+    __device__ __forceinline__ float hi() const { float a, b; get(a, b); return b; }
+};
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return r;
+}
+
+// a b, rounded, also where it is added to something next: the assembler fuses a packed
+// product and sum (seen in a result's last bit), but not this.
+__device__ __forceinline__ Pair product(Pair a, Pair b) { return fma2(a, b, Pair(0.0f)); }
+
 // The scale of a block of a given largest magnitude, and its inverse: powers of two, so that
 // scaling rounds nothing.
 template <typename Code>
@@ -50,10 +82,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ float block_max(const float *x) {
-    const float lane = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], 0.0f));
-    float r;
-    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(lane));
+__device__ __forceinline__ float block_max(const Pair *x) {
+    float t = 0.0f, r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = max3(x[i].lo(), x[i].hi(), t);
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(t));
     return r;
 }
 
@@ -76,66 +109,66 @@ __device__ __forceinline__ uint32_t pack_e5m2(float a, float b) {
     asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
     return r;
 }
-__device__ __forceinline__ float2 half2_to_float2(uint32_t h) {
-    float2 r;
+__device__ __forceinline__ Pair half2_to_pair(uint32_t h) {
+    float lo, hi;
     asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}"
-        : "=f"(r.x), "=f"(r.y) : "r"(h));
-    return r;
-}
-__device__ __forceinline__ float2 unpack_e4m3(uint32_t two) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
-    return half2_to_float2(h);
-}
-__device__ __forceinline__ float2 unpack_e5m2(uint32_t four, int upper) {        // e5m2 is fp16's upper half
-    return half2_to_float2(__byte_perm(four, 0u, upper ? 0x3424 : 0x1404));
+        : "=f"(lo), "=f"(hi) : "r"(h));
+    return Pair(lo, hi);
 }
 
 // Eight codes of a lane to values: the codes times scale.
-__device__ __forceinline__ void decode_m(uint2 c, float scale, float *m) {
+__device__ __forceinline__ void decode_m(uint2 c, float scale, Pair *m) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 t = unpack_e4m3((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
-        m[2 * i] = t.x * scale;
-        m[2 * i + 1] = t.y * scale;
+        const uint32_t two = (i < 2 ? c.x : c.y) >> (16 * (i & 1));
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
+        m[i] = product(half2_to_pair(h), Pair(scale));
     }
 }
-__device__ __forceinline__ void decode_v(uint2 c, float scale, float *v) {
+__device__ __forceinline__ void decode_v(uint2 c, float scale, Pair *v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 t = unpack_e5m2((i < 2 ? c.x : c.y), i & 1);
-        v[2 * i] = t.x * scale;
-        v[2 * i + 1] = t.y * scale;
-    }
+    for (int i = 0; i < 4; ++i)                      // e5m2 is fp16's upper half
+        v[i] = product(half2_to_pair(__byte_perm(i < 2 ? c.x : c.y, 0u, i & 1 ? 0x3424 : 0x1404)), Pair(scale));
 }
 
 // A block's eight values in each lane to codes and the block's scale.  RANDOM: rounded with the
 // random word times each place's constant, else to nearest.  The whole warp calls it.
 template <bool RANDOM>
-__device__ __forceinline__ uint2 encode_m(const float *m, uint32_t word, float &scale) {
-    float inverse, y[8];
+__device__ __forceinline__ uint2 encode_m(const Pair *m, uint32_t word, float &scale) {
+    float inverse;
     block_scale<CodeM>(block_max(m), scale, inverse);
+    uint32_t two[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        y[i] = m[i] * inverse;
-        // what is too small to count must not meet the move: it would borrow from the sign
-        if (RANDOM && fabsf(y[i]) >= 0x1p-30f) y[i] = moved<CodeM>(y[i], word * place_odd(i));
+    for (int i = 0; i < 4; ++i) {
+        float y[2];
+        (m[i] * Pair(inverse)).get(y[0], y[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            // what is too small to count must not meet the move: it would borrow from the sign
+            if (RANDOM && fabsf(y[k]) >= 0x1p-30f) y[k] = moved<CodeM>(y[k], word * place_odd(2 * i + k));
+        two[i] = pack_e4m3(y[0], y[1]);
     }
-    return make_uint2(pack_e4m3(y[0], y[1]) | pack_e4m3(y[2], y[3]) << 16,
-                      pack_e4m3(y[4], y[5]) | pack_e4m3(y[6], y[7]) << 16);
+    return make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
 }
 template <bool RANDOM>
-__device__ __forceinline__ uint2 encode_v(const float *v, uint32_t word, float &scale) {
-    float inverse, y[8];
+__device__ __forceinline__ uint2 encode_v(const Pair *v, uint32_t word, float &scale) {
+    float inverse;
     block_scale<CodeV>(block_max(v), scale, inverse);
     if (inverse == 0.0f) return make_uint2(0u, 0u);
+    uint32_t two[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        y[i] = fmaxf(v[i] * inverse, 0x1p-16f);
-        if (RANDOM) y[i] = moved<CodeV>(y[i], word * place_odd(i));
+    for (int i = 0; i < 4; ++i) {
+        float y[2];
+        (v[i] * Pair(inverse)).get(y[0], y[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            y[k] = fmaxf(y[k], 0x1p-16f);
+            if (RANDOM) y[k] = moved<CodeV>(y[k], word * place_odd(2 * i + k));
+        }
+        two[i] = pack_e5m2(y[0], y[1]);
     }
-    return make_uint2(pack_e5m2(y[0], y[1]) | pack_e5m2(y[2], y[3]) << 16,
-                      pack_e5m2(y[4], y[5]) | pack_e5m2(y[6], y[7]) << 16);
+    return make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
 }
 
 }  // namespace mtdao
