@@ -144,64 +144,71 @@ __device__ __forceinline__ float ema(float c, float s, float target) {
     return isinf(s) && c < 1.0f ? fmaf(c, target, s) : fmaf(c, target, fmaf(-c, s, s));
 }
 
-// One block of 256 elements a warp.  In 8 bits m and v are formed with a rounding
-// after each operation: what the formula gives then does not depend on a compiler's
-// choice of fused operations, and a test can ask for its very codes.  beta multiplies the
-// block's scale, a power of two, rather than each value.  The square root and the
-// reciprocal are the hardware's (2^-22): their error is far below an update's effect on p.
-template <int BITS, bool CLIP>
-__global__ void __launch_bounds__(kAdamwThreads, 5) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
-                                                                   const float *clip_scale) {
-    __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
-    const uint32_t replica = blockIdx.y;
-    const AdamwChunk c = load_chunk(a.chunks + replica * a.n_chunks + blockIdx.x);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (warp * kAdamwBlock >= c.n) return;
-    const int at = warp * kAdamwBlock + 8 * lane;
+constexpr int kAhead = kAdamwLongChunk / kAdamwChunk;       // blocks of a long record that one warp takes
+
+// What a warp reads of one block of 256 elements.
+template <int BITS>
+struct Raw {
+    uint32_t g[8], p[8];
+    uint2 cm, cv;                 // 8 bits
+    float scale_m, scale_v;
+    Pair m[4], v[4];              // 32 bits
+};
+
+// Everything that a block's update reads, before any arithmetic.
+template <int BITS>
+__device__ __forceinline__ void load_block(const AdamwList &a, const AdamwChunk &c, int warp, uint32_t *stage, Raw<BITS> &r) {
+    const int lane = threadIdx.x & 31, at = warp * kAdamwBlock + 8 * lane;
     const uint32_t block = c.block + warp;
     const int64_t eight = static_cast<int64_t>(block) * (kAdamwBlock / 8) + lane;   // the lane's, in groups of eight
-    const bool p16 = (c.flags & kAdamwParamBf16) != 0, g16 = (c.flags & kAdamwGradBf16) != 0;
-    const bool full = (warp + 1) * kAdamwBlock <= c.n;
-    const bool p_whole = full && (c.flags & kAdamwParamAligned), g_whole = full && (c.flags & kAdamwGradAligned);
-
-    // every load before any arithmetic
-    uint32_t gw[8], pw[8];
-    Pair m[4], v[4];
-    uint2 cm, cv;
-    float scale_m, scale_v;
     if constexpr (BITS == 8) {
-        cm = __ldcs(static_cast<const uint2 *>(a.m) + eight);
-        cv = __ldcs(static_cast<const uint2 *>(a.v) + eight);
-        scale_m = __ldcs(a.m_scale + block);
-        scale_v = __ldcs(a.v_scale + block);
+        r.cm = __ldcs(static_cast<const uint2 *>(a.m) + eight);
+        r.cv = __ldcs(static_cast<const uint2 *>(a.v) + eight);
+        r.scale_m = __ldcs(a.m_scale + block);
+        r.scale_v = __ldcs(a.v_scale + block);
     } else {
-        load_pairs(static_cast<const float *>(a.m) + 8 * eight, m);
-        load_pairs(static_cast<const float *>(a.v) + 8 * eight, v);
+        load_pairs(static_cast<const float *>(a.m) + 8 * eight, r.m);
+        load_pairs(static_cast<const float *>(a.v) + 8 * eight, r.v);
     }
-    load_raw(c.g, g16, g_whole, at, c.n, stages[warp], gw);
-    load_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
-    const float s = CLIP ? clip_scale[replica] : 1.0f;
+    const bool full = (warp + 1) * kAdamwBlock <= c.n;
+    load_raw(c.g, c.flags & kAdamwGradBf16, full && (c.flags & kAdamwGradAligned), at, c.n, stage, r.g);
+    load_raw(c.p, c.flags & kAdamwParamBf16, full && (c.flags & kAdamwParamAligned), at, c.n, stage, r.p);
+}
+
+// FAST: bf16 parameters and gradients, aligned, a full block.
+// In 8 bits m and v are formed with a rounding after each operation: what the formula
+// gives then does not depend on a compiler's choice of fused operations, and a test can ask
+// for its very codes.  beta multiplies the block's scale, a power of two, rather than
+// each value.  The square root and the reciprocal are the hardware's (2^-22 together): their error is
+// far below what p's own rounding leaves.
+template <int BITS, bool CLIP, bool FAST>
+__device__ __forceinline__ void update_block(const AdamwList &a, const AdamwScalars &sc, const AdamwChunk &c, uint32_t replica,
+                                             float s, int warp, uint32_t *stage, Raw<BITS> &r) {
+    const int lane = threadIdx.x & 31, at = warp * kAdamwBlock + 8 * lane;
+    const uint32_t block = c.block + warp;
+    const int64_t eight = static_cast<int64_t>(block) * (kAdamwBlock / 8) + lane;
+    const bool p16 = FAST || (c.flags & kAdamwParamBf16);
     const float keep = fmaf(-sc.decay, c.decay, 1.0f);
     Pair g[4], p[4];
-    to_pairs(gw, g16, g);
-    to_pairs(pw, p16, p);
+    to_pairs(r.g, FAST || (c.flags & kAdamwGradBf16), g);
+    to_pairs(r.p, p16, p);
     if constexpr (BITS == 8) {
-        decode_m(cm, sc.b1 * scale_m, m);
-        decode_v(cv, sc.b2 * scale_v, v);
+        decode_m(r.cm, sc.b1 * r.scale_m, r.m);
+        decode_v(r.cv, sc.b2 * r.scale_v, r.v);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if constexpr (CLIP) g[i] = product(g[i], Pair(s));
         if constexpr (BITS == 8) {
-            m[i] = m[i] + product(g[i], Pair(sc.c1));
-            v[i] = v[i] + product(g[i] * g[i], Pair(sc.c2));
+            r.m[i] = r.m[i] + product(g[i], Pair(sc.c1));
+            r.v[i] = r.v[i] + product(g[i] * g[i], Pair(sc.c2));
         } else {
             const Pair q = g[i] * g[i];
-            m[i] = Pair(ema(sc.c1, m[i].lo(), g[i].lo()), ema(sc.c1, m[i].hi(), g[i].hi()));
-            v[i] = Pair(ema(sc.c2, v[i].lo(), q.lo()), ema(sc.c2, v[i].hi(), q.hi()));
+            r.m[i] = Pair(ema(sc.c1, r.m[i].lo(), g[i].lo()), ema(sc.c1, r.m[i].hi(), g[i].hi()));
+            r.v[i] = Pair(ema(sc.c2, r.v[i].lo(), q.lo()), ema(sc.c2, r.v[i].hi(), q.hi()));
         }
-        const Pair d = fma2(Pair(sqrt_approx(v[i].lo()), sqrt_approx(v[i].hi())), Pair(sc.root), Pair(sc.eps));
-        p[i] = fma2(m[i] * Pair(-sc.step), Pair(rcp_approx(d.lo()), rcp_approx(d.hi())), p[i] * Pair(keep));
+        const Pair d = fma2(Pair(sqrt_approx(r.v[i].lo()), sqrt_approx(r.v[i].hi())), Pair(sc.root), Pair(sc.eps));
+        p[i] = fma2(r.m[i] * Pair(-sc.step), Pair(rcp_approx(d.lo()), rcp_approx(d.hi())), p[i] * Pair(keep));
     }
     uint32_t low = 0, high = 0;
     if (BITS == 8 || p16) {
@@ -211,84 +218,202 @@ __global__ void __launch_bounds__(kAdamwThreads, 5) adamw_step_kernel(const Adam
         low = static_cast<uint32_t>(z);
         high = static_cast<uint32_t>(z >> 32);
     }
+    uint32_t w[8];
     if (p16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            pw[i] = upper_halves(bf16_random(p[i].lo(), low * place_odd(2 * i)),
-                                 bf16_random(p[i].hi(), low * place_odd(2 * i + 1)));
+            w[i] = upper_halves(bf16_random(p[i].lo(), low * place_odd(2 * i)),
+                                bf16_random(p[i].hi(), low * place_odd(2 * i + 1)));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pw[i] = __float_as_uint(i & 1 ? p[i / 2].hi() : p[i / 2].lo());
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(i & 1 ? p[i / 2].hi() : p[i / 2].lo());
     }
-    store_raw(c.p, p16, p_whole, at, c.n, stages[warp], pw);
+    const bool whole = FAST || ((warp + 1) * kAdamwBlock <= c.n && (c.flags & kAdamwParamAligned));
+    store_raw(c.p, p16, whole, at, c.n, stage, w);
     if constexpr (BITS == 8) {
-        cm = encode_m<true>(m, low, scale_m);
+        float scale_m, scale_v;
+        const uint2 cm = encode_m<true>(r.m, low, scale_m);
         __stcs(static_cast<uint2 *>(a.m) + eight, cm);
-        cv = encode_v<true>(v, high, scale_v);
+        const uint2 cv = encode_v<true>(r.v, high, scale_v);
         __stcs(static_cast<uint2 *>(a.v) + eight, cv);
         if (lane == 0) {
             a.m_scale[block] = scale_m;
             a.v_scale[block] = scale_v;
         }
     } else {
-        store_pairs(static_cast<float *>(a.m) + 8 * eight, m);
-        store_pairs(static_cast<float *>(a.v) + 8 * eight, v);
+        store_pairs(static_cast<float *>(a.m) + 8 * eight, r.m);
+        store_pairs(static_cast<float *>(a.v) + 8 * eight, r.v);
+    }
+}
+
+// Copies to shared memory that run while the thread goes on; each lane later reads what it
+// copied itself, so that waiting for its own copies is all that it takes.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *to, const void *from) {
+    const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(at), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(at), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(LATER) : "memory"); }
+
+// A warp's blocks of one record, on their way from memory.
+struct Ahead {
+    uint4 g[32], p[32];
+    uint2 cm[32], cv[32];
+};
+
+template <int BITS, bool CLIP>
+__global__ void __launch_bounds__(kAdamwThreads, 4) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
+                                                                      const float *clip_scale) {
+    constexpr int kWarps = kAdamwThreads / 32;
+    constexpr uint32_t kFast = kAdamwParamBf16 | kAdamwGradBf16 | kAdamwParamAligned | kAdamwGradAligned;
+    union Shared {
+        uint32_t stage[kAdamwBlock];
+        Ahead ahead[BITS == 8 ? kAhead : 1];
+    };
+    __shared__ __align__(16) Shared shared[kWarps];
+    const uint32_t replica = blockIdx.y;
+    const AdamwChunk c = load_chunk(a.chunks + replica * a.n_chunks + blockIdx.x);
+    int warp = threadIdx.x >> 5;                        // the block of the record that this warp is at
+    Shared &mine = shared[warp];
+    if constexpr (BITS == 8) {
+        const int lane = threadIdx.x & 31, full = c.n / kAdamwBlock;
+        if ((c.flags & kFast) == kFast && warp < full) {
+            // everything that the warp needs of the record is asked for at once
+            float scales = 0.0f;
+            if (lane < 2 * kAhead) {
+                const int b = warp + (lane >> 1) * kWarps;
+                if (b < full) scales = __ldcs((lane & 1 ? a.v_scale : a.m_scale) + c.block + b);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int b = warp + i * kWarps;
+                if (b < full) {
+                    const int64_t eight = static_cast<int64_t>(c.block + b) * (kAdamwBlock / 8) + lane;
+                    copy_async<16>(&mine.ahead[i].g[lane], static_cast<const uint4 *>(c.g) + b * 32 + lane);
+                    copy_async<16>(&mine.ahead[i].p[lane], static_cast<const uint4 *>(c.p) + b * 32 + lane);
+                    copy_async<8>(&mine.ahead[i].cm[lane], static_cast<const uint2 *>(a.m) + eight);
+                    copy_async<8>(&mine.ahead[i].cv[lane], static_cast<const uint2 *>(a.v) + eight);
+                }
+                copies_commit();
+            }
+            const float s = CLIP ? clip_scale[replica] : 1.0f;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (warp >= full) break;
+                switch (i) {
+                    case 0: copies_wait<kAhead - 1>(); break;
+                    case 1: copies_wait<kAhead - 2>(); break;
+                    case 2: copies_wait<kAhead - 3>(); break;
+                    default: copies_wait<0>(); break;
+                }
+                Raw<BITS> r;
+                const uint4 g = mine.ahead[i].g[lane], p = mine.ahead[i].p[lane];
+                r.g[0] = g.x, r.g[1] = g.y, r.g[2] = g.z, r.g[3] = g.w;
+                r.p[0] = p.x, r.p[1] = p.y, r.p[2] = p.z, r.p[3] = p.w;
+                r.cm = mine.ahead[i].cm[lane];
+                r.cv = mine.ahead[i].cv[lane];
+                r.scale_m = __shfl_sync(0xffffffffu, scales, 2 * i);
+                r.scale_v = __shfl_sync(0xffffffffu, scales, 2 * i + 1);
+                update_block<BITS, CLIP, true>(a, sc, c, replica, s, warp, nullptr, r);
+                warp += kWarps;
+            }
+            copies_wait<0>();
+            __syncwarp();
+        }
+    }
+    const float s = CLIP ? clip_scale[replica] : 1.0f;
+    for (; warp * kAdamwBlock < c.n; warp += kWarps) {
+        Raw<BITS> r;
+        load_block<BITS>(a, c, warp, mine.stage, r);
+        update_block<BITS, CLIP, false>(a, sc, c, replica, s, warp, mine.stage, r);
     }
 }
 
 // ---------------------------------------------------------------- gradient norms
 
-__global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const AdamwList a, double *partial) {
-    const int replica = blockIdx.y;
-    const AdamwChunk *chunks = a.chunks + replica * a.n_chunks;
-    __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
-    const int warp = threadIdx.x >> 5;
-    Kahan sum;
-    double wide = 0.0;
-    for (int64_t k = blockIdx.x; k < a.n_chunks; k += gridDim.x) {
-        const AdamwChunk c = load_chunk(chunks + k);
-        const bool g16 = (c.flags & kAdamwGradBf16) != 0;
-        const bool whole = (warp + 1) * kAdamwBlock <= c.n && (c.flags & kAdamwGradAligned);
-        uint32_t gw[8];
-        load_raw(c.g, g16, whole, 8 * threadIdx.x, c.n, stages[warp], gw);
-        Pair gp[4], qp = Pair(0.0f);
-        to_pairs(gw, g16, gp);
-        float g[8];
+// Sum of squares of a lane's eight values of a block, as bits: into sum, or
+// into wide where fp32 does not hold the squares.
+__device__ __forceinline__ void add_squares(const uint32_t *w, bool bf16, Kahan &sum, double &wide) {
+    Pair x[4], q = Pair(0.0f);
+    to_pairs(w, bf16, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            qp = fma2(gp[i], gp[i], qp);
-            gp[i].get(g[2 * i], g[2 * i + 1]);
-        }
-        const float q = qp.lo() + qp.hi();
-        if (q >= 0x1p-90f && q <= 0x1p100f) {
-            sum.add(q);
-        } else {                                     // zeros, or squares that fp32 does not hold
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (g[i] != 0.0f) wide = fma(static_cast<double>(g[i]), static_cast<double>(g[i]), wide);
-        }
+    for (int i = 0; i < 4; ++i) q = fma2(x[i], x[i], q);
+    const float both = q.lo() + q.hi();
+    if (both >= 0x1p-90f && both <= 0x1p100f) {
+        sum.add(both);
+        return;
     }
-    __shared__ double sums[kAdamwThreads / 32];
-    const double w = warp_sum(sum.value() + wide);
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = w;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double t = 0.0;
-        for (int i = 0; i < kAdamwThreads / 32; ++i) t += sums[i];
-        partial[static_cast<int64_t>(replica) * gridDim.x + blockIdx.x] = t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const double t = i & 1 ? x[i / 2].hi() : x[i / 2].lo();
+        if (t != 0.0) wide = fma(t, t, wide);
     }
 }
 
-__global__ void __launch_bounds__(32) adamw_norm_last_kernel(const double *partial, int blocks, double *sums, float *scale,
-                                                             double max_norm) {
+// The blocks of a replica take its records in turn; each record's loads go out together, and
+// the next record's addresses with them.  The replica's last block adds the blocks' sums, in their order.
+__global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const AdamwList a, double *partial, uint32_t *arrived,
+                                                                   double *sums, float *scale, double max_norm) {
+    constexpr int kWarps = kAdamwThreads / 32;
+    __shared__ __align__(16) uint32_t stages[kWarps][kAdamwBlock];
+    const int replica = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const AdamwChunk *chunks = a.chunks + replica * a.n_chunks;
+    Kahan sum;
+    double wide = 0.0;
+    AdamwChunk next = load_chunk(chunks + blockIdx.x);
+    for (int64_t k = blockIdx.x; k < a.n_chunks; k += gridDim.x) {
+        const AdamwChunk c = next;
+        if (k + gridDim.x < a.n_chunks) next = load_chunk(chunks + k + gridDim.x);
+        const bool g16 = (c.flags & kAdamwGradBf16) != 0;
+        const int whole = c.flags & kAdamwGradAligned ? c.n / kAdamwBlock : 0;
+        uint32_t w[kAhead][8];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int b = warp + i * kWarps;
+            if (b < whole) load_raw(c.g, g16, true, b * kAdamwBlock + 8 * lane, c.n, nullptr, w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int b = warp + i * kWarps;
+            if (b * kAdamwBlock >= c.n) break;
+            if (b >= whole) load_raw(c.g, g16, false, b * kAdamwBlock + 8 * lane, c.n, stages[warp], w[i]);
+            add_squares(w[i], g16, sum, wide);
+        }
+    }
+    __shared__ double parts[kWarps];
+    __shared__ bool last;
+    const double in_warp = warp_sum(sum.value() + wide);
+    if (lane == 0) parts[warp] = in_warp;
+    __syncthreads();
+    double *mine = partial + static_cast<int64_t>(replica) * gridDim.x;
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int i = 0; i < kWarps; ++i) t += parts[i];
+        __stcg(mine + blockIdx.x, t);
+        __threadfence();
+        last = atomicAdd(arrived + replica, 1u) + 1u == gridDim.x;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
     double t = 0.0;
-    for (int i = threadIdx.x; i < blocks; i += 32) t += partial[static_cast<int64_t>(blockIdx.x) * blocks + i];
+    for (int i = threadIdx.x; i < static_cast<int>(gridDim.x); i += kAdamwThreads) t += __ldcg(mine + i);
     t = warp_sum(t);
+    if (lane == 0) parts[warp] = t;
+    __syncthreads();
     if (threadIdx.x != 0) return;
-    if (sums) sums[blockIdx.x] = t;
+    t = 0.0;
+    for (int i = 0; i < kWarps; ++i) t += parts[i];
+    arrived[replica] = 0;                              // for the next launch
+    if (sums) sums[replica] = t;
     if (scale) {
         const double s = max_norm / (sqrt(t) + 1e-6);
-        scale[blockIdx.x] = static_cast<float>(s > 1.0 ? 1.0 : s);       // a NaN stays one
+        scale[replica] = static_cast<float>(s > 1.0 ? 1.0 : s);          // a NaN stays one
     }
 }
 
@@ -333,8 +458,9 @@ template <int BITS>
 __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const AdamwList a, uint32_t mask) {
     __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
     const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (warp * kAdamwBlock >= c.n) return;
+    const int lane = threadIdx.x & 31;
+    for (int warp = threadIdx.x >> 5; warp * kAdamwBlock < c.n; warp += kAdamwThreads / 32) {
+    uint32_t *stage = stages[threadIdx.x >> 5];
     const int at = warp * kAdamwBlock + 8 * lane;
     const int64_t blocks = a.n_state / kAdamwBlock;
     const int64_t block = c.block + warp;
@@ -346,7 +472,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
         uint32_t w[8];
         mean8(a.M, [&](int r, Pair *s) {
             const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
-            load_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stages[warp], w);
+            load_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stage, w);
             to_pairs(w, p16, s);
         }, mean);
 #pragma unroll
@@ -357,7 +483,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
         }
         for (int r = 0; r < a.M; ++r) {
             const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
-            store_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stages[warp], w);
+            store_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stage, w);
         }
     }
 #pragma unroll
@@ -383,6 +509,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
             for (int r = 0; r < a.M; ++r) store_pairs(s32 + r * a.n_state + e, mean);
         }
     }
+    }
 }
 
 // ---------------------------------------------------------------- records
@@ -390,7 +517,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
 __global__ void __launch_bounds__(kAdamwThreads) adamw_bind_kernel(AdamwChunk *chunks, const AdamwTensor *tensors,
                                                                    int32_t n_tensors, void *const *table,
                                                                    const int32_t *dtype, bool grads, int64_t n_chunks,
-                                                                   int64_t n_blocks) {
+                                                                   int32_t chunk, int64_t n_blocks) {
     const int64_t k = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
     if (k >= n_chunks) return;
     int32_t lo = 0, hi = n_tensors;                  // the last tensor whose first chunk is at most k: an empty
@@ -399,7 +526,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_bind_kernel(AdamwChunk *c
         if (tensors[mid].first_chunk <= k) lo = mid; else hi = mid;
     }
     const AdamwTensor t = tensors[lo];
-    const int64_t first = (k - t.first_chunk) * kAdamwChunk;
+    const int64_t first = (k - t.first_chunk) * chunk;
     const bool bf16 = dtype[lo] == MTDAO_BF16;
     AdamwChunk &c = chunks[blockIdx.y * n_chunks + k];
     char *p = static_cast<char *>(table[static_cast<int64_t>(blockIdx.y) * n_tensors + lo]) + first * (bf16 ? 2 : 4);
@@ -413,7 +540,7 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_bind_kernel(AdamwChunk *c
     const int64_t left = t.numel - first;
     c.p = p;
     c.block = static_cast<uint32_t>(blockIdx.y * n_blocks + t.first_block + first / kAdamwBlock);
-    c.n = static_cast<int32_t>(left < kAdamwChunk ? left : kAdamwChunk);
+    c.n = static_cast<int32_t>(left < chunk ? left : chunk);
     c.flags = (c.flags & ~(kAdamwParamBf16 | kAdamwParamAligned)) | (bf16 ? kAdamwParamBf16 : 0u) |
               (aligned ? kAdamwParamAligned : 0u);
     c.decay = t.decay;
@@ -422,12 +549,16 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_bind_kernel(AdamwChunk *c
 }  // namespace
 
 cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, int32_t n_tensors, void *const *table,
-                              const int32_t *dtype, bool grads, int64_t n_chunks, int64_t n_blocks, int32_t M,
-                              cudaStream_t stream) {
+                              const int32_t *dtype, bool grads, int64_t n_chunks, int32_t chunk, int64_t n_blocks,
+                              int32_t M, cudaStream_t stream) {
     const dim3 grid(static_cast<unsigned>((n_chunks + kAdamwThreads - 1) / kAdamwThreads), M);
     adamw_bind_kernel<<<grid, kAdamwThreads, 0, stream>>>(chunks, tensors, n_tensors, table, dtype, grads, n_chunks,
-                                                          n_blocks);
+                                                          chunk, n_blocks);
     return cudaGetLastError();
+}
+
+int32_t adamw_chunk(int num_sms, int bits, int64_t elements) {
+    return bits == 8 && elements >= static_cast<int64_t>(num_sms) * 8 * kAdamwLongChunk ? kAdamwLongChunk : kAdamwChunk;
 }
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {
@@ -439,14 +570,13 @@ cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const 
 }
 
 int adamw_norm_blocks(int num_sms, int M, int64_t n_chunks) {
-    const int64_t want = (8 * static_cast<int64_t>(num_sms) + M - 1) / M;
+    const int64_t want = (6 * static_cast<int64_t>(num_sms) + M - 1) / M;
     return static_cast<int>(n_chunks < want ? n_chunks : want);
 }
 
-cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, double *sums, float *scale,
-                              double max_norm, cudaStream_t stream) {
-    adamw_norm_kernel<<<dim3(blocks, a.M), kAdamwThreads, 0, stream>>>(a, partial);
-    adamw_norm_last_kernel<<<a.M, 32, 0, stream>>>(partial, blocks, sums, scale, max_norm);
+cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, uint32_t *arrived, double *sums,
+                              float *scale, double max_norm, cudaStream_t stream) {
+    adamw_norm_kernel<<<dim3(blocks, a.M), kAdamwThreads, 0, stream>>>(a, partial, arrived, sums, scale, max_norm);
     return cudaGetLastError();
 }
 

@@ -9,17 +9,20 @@
 namespace mtdao {
 
 constexpr int kAdamwBlock = MTDAO_ADAMW_BLOCK;   // elements that share a scale: one warp's
-constexpr int kAdamwChunk = 2048;                // elements of one record: one thread block's
 constexpr int kAdamwThreads = 256;
 
-// A stretch of one tensor of one replica, as the kernels walk the list: up to
-// kAdamwChunk elements, so that a thread block finds its addresses with one
-// load of 32 bytes (0.2 % of what a step moves).
+// Elements of one record, which is one thread block's work: a block of kAdamwBlock for each warp,
+// or several one after another (adamw_chunk).
+constexpr int kAdamwChunk = kAdamwThreads / 32 * kAdamwBlock;
+constexpr int kAdamwLongChunk = 4 * kAdamwChunk;
+
+// A stretch of one tensor of one replica, as the kernels walk the list, so that
+// a thread block finds its addresses with one load of 32 bytes (0.2 % of what a step moves, or less).
 struct __align__(16) AdamwChunk {
     void *p;                  // first element of the parameters
     const void *g;            // and of the gradients
     uint32_t block;           // its first state block, counted over all replicas
-    int32_t n;                // 1 .. kAdamwChunk elements
+    int32_t n;                // elements, 1 .. AdamwList::chunk
     uint32_t flags;           // kAdamw*
     float decay;              // the tensor's decay factor
 };
@@ -31,6 +34,7 @@ constexpr uint32_t kAdamwParamAligned = 4, kAdamwGradAligned = 8;
 struct AdamwList {
     const AdamwChunk *chunks;    // [M][n_chunks]
     int64_t n_chunks;            // of one replica
+    int32_t chunk;               // elements of a record that is not its tensor's last
     int64_t n_state;             // elements of one replica's state vector
     int32_t M;
     int32_t bits;                // 32 or 8
@@ -57,16 +61,19 @@ struct AdamwTensor {
 
 // Writes the addresses in table [M][n_tensors] (and what else belongs to the parameters) into the records.
 cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, int32_t n_tensors, void *const *table,
-                              const int32_t *dtype, bool grads, int64_t n_chunks, int64_t n_blocks, int32_t M,
-                              cudaStream_t stream);
+                              const int32_t *dtype, bool grads, int64_t n_chunks, int32_t chunk, int64_t n_blocks,
+                              int32_t M, cudaStream_t stream);
+
+// The record's length for a list of so many elements over all replicas.
+int32_t adamw_chunk(int num_sms, int bits, int64_t elements);
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream);
 
 // ||g||^2 of each replica into sums[M] (fixed order) and, where scale is not
 // NULL, min(1, max_norm / (||g|| + 1e-6)) into scale[M].  partial holds M *
-// adamw_norm_blocks() doubles.
+// adamw_norm_blocks() doubles, arrived M counters, zero before and after.
 int adamw_norm_blocks(int num_sms, int M, int64_t n_chunks);
-cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, double *sums, float *scale,
-                              double max_norm, cudaStream_t stream);
+cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, uint32_t *arrived, double *sums,
+                              float *scale, double max_norm, cudaStream_t stream);
 cudaError_t launch_adamw_average(const AdamwList &a, uint32_t mask, cudaStream_t stream);
 
 }  // namespace mtdao

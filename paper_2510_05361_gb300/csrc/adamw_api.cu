@@ -31,7 +31,8 @@ struct mtdao_adamw_ctx {
     void **table = nullptr;              // [M][n_tensors], scratch of a binding
     int32_t *dtypes = nullptr;           // [n_tensors], likewise
     int norm_blocks = 1;
-    double *norm_partial = nullptr, *norm_sums = nullptr;
+    double *norm_partial = nullptr;
+    uint32_t *norm_arrived = nullptr;
     float *clip_scale = nullptr;
     int device = 0;
     cudaStream_t stream = nullptr;
@@ -84,33 +85,38 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
     h->cfg = *cfg;
     h->n_tensors = n_tensors;
     h->tensors.resize(n_tensors);
-    int64_t chunks = 0, blocks = 0;
+    int64_t elements = 0;
     for (int32_t k = 0; k < n_tensors; ++k) {
-        if (numel[k] < 0 || numel[k] > (int64_t(1) << 40))
-            return fail(nullptr, MTDAO_ERR_INVALID, "tensor %d has numel %lld", k, static_cast<long long>(numel[k]));
+        if (numel[k] < 0 || numel[k] > (int64_t(1) << 40) || (elements += numel[k]) > (int64_t(1) << 40))
+            return fail(nullptr, MTDAO_ERR_INVALID, "tensor %d has numel %lld, or the list over 2^40 elements", k,
+                        static_cast<long long>(numel[k]));
         const float d = decay ? decay[k] : 1.0f;
         if (!(std::isfinite(d) && d >= 0.0f))
             return fail(nullptr, MTDAO_ERR_INVALID, "decay[%d]=%g must be finite and not negative", k, d);
-        h->tensors[k] = {numel[k], chunks, blocks, d, 0};
-        chunks += (numel[k] + kAdamwChunk - 1) / kAdamwChunk;
-        blocks += (numel[k] + kAdamwBlock - 1) / kAdamwBlock;
-        if (blocks > 0xffffffffll) break;
     }
-    if (blocks == 0) return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list holds no element");
-    // the records count blocks in 32 bits, a grid a replica's chunks in 31, the random numbers groups of 8 in 32
-    if (blocks * M > 0xffffffffll || chunks > 0x7fffffffll || blocks * (kAdamwBlock / 8) > 0xffffffffll)
-        return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list is too long for %d replicas", M);
-
+    if (elements == 0) return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list holds no element");
     h->stream = static_cast<cudaStream_t>(cuda_stream);
     int sms = 1;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
     if (e != cudaSuccess) return cuda_fail(nullptr, e, "no usable CUDA device");
 
+    const int32_t chunk = adamw_chunk(sms, cfg->state_bits, elements * M);
+    int64_t chunks = 0, blocks = 0;
+    for (int32_t k = 0; k < n_tensors; ++k) {
+        h->tensors[k] = {numel[k], chunks, blocks, decay ? decay[k] : 1.0f, 0};
+        chunks += (numel[k] + chunk - 1) / chunk;
+        blocks += (numel[k] + kAdamwBlock - 1) / kAdamwBlock;
+    }
+    // the records count blocks in 32 bits, a grid a replica's chunks in 31, the random numbers groups of 8 in 32
+    if (blocks * M > 0xffffffffll || chunks > 0x7fffffffll || blocks * (kAdamwBlock / 8) > 0xffffffffll)
+        return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list is too long for %d replicas", M);
+
     AdamwList &a = h->list;
     a.M = M;
     a.bits = cfg->state_bits;
     a.n_chunks = chunks;
+    a.chunk = chunk;
     a.n_state = blocks * kAdamwBlock;
     h->norm_blocks = adamw_norm_blocks(sms, M, chunks);
     const size_t held = static_cast<size_t>(M) * a.n_state * (a.bits / 8);
@@ -128,7 +134,7 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
         {reinterpret_cast<void **>(&h->table), static_cast<size_t>(M) * n_tensors * sizeof(void *)},
         {reinterpret_cast<void **>(&h->dtypes), n_tensors * sizeof(int32_t)},
         {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(M) * h->norm_blocks * sizeof(double)},
-        {reinterpret_cast<void **>(&h->norm_sums), M * sizeof(double)},
+        {reinterpret_cast<void **>(&h->norm_arrived), M * sizeof(uint32_t)},
         {reinterpret_cast<void **>(&h->clip_scale), M * sizeof(float)},
     };
     // one allocation: a call to the driver costs more than setting up a small list
@@ -183,7 +189,7 @@ int upload(mtdao_adamw_ctx *h, void *const *table, const int32_t *dtype, bool gr
         e = cudaMemcpyAsync(h->dtypes, dtype, h->n_tensors * sizeof(int32_t), cudaMemcpyHostToDevice, h->stream);
     if (e == cudaSuccess)
         e = launch_adamw_bind(h->chunks, h->tensors_dev, h->n_tensors, h->table, h->dtypes, grads, a.n_chunks,
-                              a.n_state / kAdamwBlock, a.M, h->stream);
+                              a.chunk, a.n_state / kAdamwBlock, a.M, h->stream);
     return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "binding tensors");
 }
 
@@ -307,7 +313,8 @@ extern "C" int mtdao_adamw_step(mtdao_adamw_handle h, double lr, double weight_d
     cudaError_t e = cudaSuccess;
     if (max_norm > 0.0) {
         scale = h->clip_scale;
-        e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, h->norm_sums, h->clip_scale, max_norm, h->stream);
+        e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, h->norm_arrived, nullptr, h->clip_scale,
+                              max_norm, h->stream);
     }
     if (e == cudaSuccess) e = launch_adamw_step(h->list, sc, scale, h->stream);
     if (e != cudaSuccess) return cuda_fail(h, e, "AdamW step");
@@ -322,7 +329,8 @@ extern "C" int mtdao_adamw_grad_sqnorm(mtdao_adamw_handle h, double *out_dev) {
     if (!h->has_grads) return fail(h, MTDAO_ERR_STATE, "grad_sqnorm: no gradients are bound");
     Range range("mtdao_adamw_grad_sqnorm");
     if (int rc = select_device(h)) return rc;
-    const cudaError_t e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, out_dev, nullptr, 0.0, h->stream);
+    const cudaError_t e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, h->norm_arrived, out_dev, nullptr,
+                                            0.0, h->stream);
     return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "gradient norm");
 }
 
