@@ -6,6 +6,8 @@
 // the block of elements that shares a scale in 8 bits, eight consecutive ones a lane: the
 // block's largest magnitude is then one warp reduction, and a step reads and
 // writes each quantity once.
+#include <algorithm>
+
 #include "adamw.h"
 #include "adamw_codes.cuh"
 #include "kahan.cuh"
@@ -39,11 +41,11 @@ __device__ __forceinline__ void store_words8(void *p, const uint32_t *w) {
 
 // A warp's 256 elements of a tensor that may be of either type and start anywhere,
 // as bits: in w[0..7] a lane's eight consecutive ones, bf16 packed in pairs
-// into w[0..3].  Full warps of aligned tensors are read 16 (bf16) or 32 bytes (fp32) a
-// lane; the others element by element, lanes side by side, and turned in shared
-// memory (stage: 256 words of the warp's own), zeros past n.
-__device__ __forceinline__ void load_raw(const void *p, bool bf16, bool whole, int at, int n, uint32_t *stage, uint32_t *w) {
-    const int lane = threadIdx.x & 31;
+// into w[0..3].  Full blocks of aligned tensors are read 16 (bf16) or 32 bytes (fp32) a
+// lane.  The others are read element by element, lanes side by side, zeros past n, and
+// turn_raw then exchanges them in shared memory (stage: 256 words of the warp's own); apart,
+// so that several tensors' loads can be under way before the first exchange.
+__device__ __forceinline__ void load_raw(const void *p, bool bf16, bool whole, int at, int n, uint32_t *w) {
     if (whole) {
         if (bf16) {
             const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + at));
@@ -53,15 +55,20 @@ __device__ __forceinline__ void load_raw(const void *p, bool bf16, bool whole, i
         }
         return;
     }
-    const int first = at - 8 * lane;
-    __syncwarp();
+    const int lane = threadIdx.x & 31, first = at - 8 * lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int k = first + 32 * i + lane;
-        uint32_t bits = 0;
-        if (k < n) bits = bf16 ? __ldcs(static_cast<const uint16_t *>(p) + k) : __ldcs(static_cast<const uint32_t *>(p) + k);
-        stage[32 * i + lane] = bits;
+        w[i] = 0;
+        if (k < n) w[i] = bf16 ? __ldcs(static_cast<const uint16_t *>(p) + k) : __ldcs(static_cast<const uint32_t *>(p) + k);
     }
+}
+__device__ __forceinline__ void turn_raw(bool bf16, bool whole, uint32_t *stage, uint32_t *w) {
+    if (whole) return;
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) stage[32 * i + lane] = w[i];
     __syncwarp();
     const uint4 a = reinterpret_cast<const uint4 *>(stage)[2 * lane], b = reinterpret_cast<const uint4 *>(stage)[2 * lane + 1];
     w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
@@ -80,9 +87,12 @@ __device__ __forceinline__ void store_raw(void *p, bool bf16, bool whole, int at
         return;
     }
     const int first = at - 8 * lane;
-    __syncwarp();
+    uint32_t t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) stage[8 * lane + i] = bf16 ? (w[i / 2] >> (16 * (i & 1))) & 0xffffu : w[i];
+    for (int i = 0; i < 8; ++i) t[i] = bf16 ? (w[i / 2] >> (16 * (i & 1))) & 0xffffu : w[i];
+    __syncwarp();
+    reinterpret_cast<uint4 *>(stage)[2 * lane] = make_uint4(t[0], t[1], t[2], t[3]);
+    reinterpret_cast<uint4 *>(stage)[2 * lane + 1] = make_uint4(t[4], t[5], t[6], t[7]);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -171,8 +181,11 @@ __device__ __forceinline__ void load_block(const AdamwList &a, const AdamwChunk 
         load_pairs(static_cast<const float *>(a.v) + 8 * eight, r.v);
     }
     const bool full = (warp + 1) * kAdamwBlock <= c.n;
-    load_raw(c.g, c.flags & kAdamwGradBf16, full && (c.flags & kAdamwGradAligned), at, c.n, stage, r.g);
-    load_raw(c.p, c.flags & kAdamwParamBf16, full && (c.flags & kAdamwParamAligned), at, c.n, stage, r.p);
+    const bool g_whole = full && (c.flags & kAdamwGradAligned), p_whole = full && (c.flags & kAdamwParamAligned);
+    load_raw(c.g, c.flags & kAdamwGradBf16, g_whole, at, c.n, r.g);
+    load_raw(c.p, c.flags & kAdamwParamBf16, p_whole, at, c.n, r.p);
+    turn_raw(c.flags & kAdamwGradBf16, g_whole, stage, r.g);
+    turn_raw(c.flags & kAdamwParamBf16, p_whole, stage, r.p);
 }
 
 // FAST: bf16 parameters and gradients, aligned, a full block.
@@ -260,87 +273,157 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int LATER>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(LATER) : "memory"); }
 
-// A warp's blocks of one record, on their way from memory.
-struct Ahead {
-    uint4 g[32], p[32];
-    uint2 cm[32], cv[32];
-};
+// In 8 bits a warp's blocks come through shared memory: all four of a long record are on their
+// way at once, which registers could not hold.  What a block takes there: each tensor's 256 elements,
+// from the 16-byte boundary before them to the one after, then the codes.
+constexpr int kStageBytes = 4 * kAdamwBlock;             // turn_raw's
 
-template <int BITS, bool CLIP>
-__global__ void __launch_bounds__(kAdamwThreads, 4) adamw_step_kernel(const AdamwList a, const AdamwScalars sc,
-                                                                      const float *clip_scale) {
+__host__ __device__ __forceinline__ int tensor_bytes(bool bf16) { return bf16 ? 512 + 16 : 1024 + 16; }
+__host__ __device__ __forceinline__ int slot_bytes(bool g16, bool p16) { return tensor_bytes(g16) + tensor_bytes(p16) + 512; }
+
+// Copies the 16-byte granules that hold a block's elements; skew is its address modulo 16.
+__device__ __forceinline__ void copy_elements(char *to, const char *from, bool bf16, int skew) {
+    const int lane = threadIdx.x & 31;
+    from -= skew;
+    copy_async<16>(to + 16 * lane, from + 16 * lane);
+    if (!bf16) copy_async<16>(to + 512 + 16 * lane, from + 512 + 16 * lane);
+    const int end = bf16 ? 512 : 1024;
+    if (skew != 0 && lane == 0) copy_async<16>(to + end, from + end);
+}
+
+// A lane's eight elements of what copy_elements brought, as load_raw and turn_raw give them.
+__device__ __forceinline__ void read_elements(const char *at, bool bf16, int skew, uint32_t *w) {
+    const int lane = threadIdx.x & 31;
+    const uint4 *q = reinterpret_cast<const uint4 *>(at) + (bf16 ? lane : 2 * lane);
+    const uint4 a = q[0];
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    if (bf16 && skew == 0) return;
+    const uint4 b = q[1];
+    w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    if (skew == 0) return;
+    uint32_t t[12] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], 0, 0, 0, 0};
+    if (!bf16) {
+        const uint4 c = q[2];
+        t[8] = c.x, t[9] = c.y, t[10] = c.z, t[11] = c.w;
+    }
+    if (skew & 8) {
+#pragma unroll
+        for (int i = 0; i < 10; ++i) t[i] = t[i + 2];
+    }
+    if (skew & 4) {
+#pragma unroll
+        for (int i = 0; i < 9; ++i) t[i] = t[i + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = skew & 2 ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
+}
+
+// A warp's blocks first, first + 8, ... below end of a record, as many on their way at a time as fit
+// into its part of shared memory.  BF16: bf16 parameters and gradients, aligned: all four.
+template <bool CLIP, bool BF16>
+__device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwScalars &sc, const AdamwChunk &c, uint32_t replica,
+                                              float s, int first, int end, char *mine) {
     constexpr int kWarps = kAdamwThreads / 32;
-    constexpr uint32_t kFast = kAdamwParamBf16 | kAdamwGradBf16 | kAdamwParamAligned | kAdamwGradAligned;
-    union Shared {
-        uint32_t stage[kAdamwBlock];
-        Ahead ahead[BITS == 8 ? kAhead : 1];
+    const int lane = threadIdx.x & 31;
+    const bool g16 = BF16 || (c.flags & kAdamwGradBf16), p16 = BF16 || (c.flags & kAdamwParamBf16);
+    const int g_skew = BF16 ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.g) & 15);
+    const int p_skew = BF16 ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.p) & 15);
+    const int p_at = tensor_bytes(g16), codes_at = p_at + tensor_bytes(p16), slot = slot_bytes(g16, p16);
+    const int fit = BF16 ? kAhead : min(kAhead, a.warp_bytes / slot);
+    float scales = 0.0f;
+    if (lane < 2 * kAhead) {
+        const int b = first + (lane >> 1) * kWarps;
+        if (b < end) scales = __ldcs((lane & 1 ? a.v_scale : a.m_scale) + c.block + b);
+    }
+    auto fetch = [&](int i, char *to) {
+        const int b = first + i * kWarps;
+        if (b < end) {
+            const int64_t eight = static_cast<int64_t>(c.block + b) * (kAdamwBlock / 8) + lane;
+            copy_elements(to, static_cast<const char *>(c.g) + b * (g16 ? 512 : 1024), g16, g_skew);
+            copy_elements(to + p_at, static_cast<const char *>(c.p) + b * (p16 ? 512 : 1024), p16, p_skew);
+            copy_async<8>(to + codes_at + 8 * lane, static_cast<const uint2 *>(a.m) + eight);
+            copy_async<8>(to + codes_at + 256 + 8 * lane, static_cast<const uint2 *>(a.v) + eight);
+        }
+        copies_commit();
     };
-    __shared__ __align__(16) Shared shared[kWarps];
-    const uint32_t replica = blockIdx.y;
-    const AdamwChunk c = load_chunk(a.chunks + replica * a.n_chunks + blockIdx.x);
-    int warp = threadIdx.x >> 5;                        // the block of the record that this warp is at
-    Shared &mine = shared[warp];
-    if constexpr (BITS == 8) {
-        const int lane = threadIdx.x & 31, full = c.n / kAdamwBlock;
-        if ((c.flags & kFast) == kFast && warp < full) {
-            // everything that the warp needs of the record is asked for at once
-            float scales = 0.0f;
-            if (lane < 2 * kAhead) {
-                const int b = warp + (lane >> 1) * kWarps;
-                if (b < full) scales = __ldcs((lane & 1 ? a.v_scale : a.m_scale) + c.block + b);
-            }
+    auto work = [&](int i, char *at) {
+        if (!BF16) __syncwarp();                       // a lane reads what its neighbours copied
+        Raw<8> r;
+        read_elements(at, g16, g_skew, r.g);
+        read_elements(at + p_at, p16, p_skew, r.p);
+        r.cm = reinterpret_cast<const uint2 *>(at + codes_at)[lane];
+        r.cv = reinterpret_cast<const uint2 *>(at + codes_at + 256)[lane];
+        r.scale_m = __shfl_sync(0xffffffffu, scales, 2 * i);
+        r.scale_v = __shfl_sync(0xffffffffu, scales, 2 * i + 1);
+        // (an exchange takes place where the block's elements came in)
+        update_block<8, CLIP, BF16>(a, sc, c, replica, s, first + i * kWarps, reinterpret_cast<uint32_t *>(at), r);
+    };
+    if constexpr (BF16) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int b = warp + i * kWarps;
-                if (b < full) {
-                    const int64_t eight = static_cast<int64_t>(c.block + b) * (kAdamwBlock / 8) + lane;
-                    copy_async<16>(&mine.ahead[i].g[lane], static_cast<const uint4 *>(c.g) + b * 32 + lane);
-                    copy_async<16>(&mine.ahead[i].p[lane], static_cast<const uint4 *>(c.p) + b * 32 + lane);
-                    copy_async<8>(&mine.ahead[i].cm[lane], static_cast<const uint2 *>(a.m) + eight);
-                    copy_async<8>(&mine.ahead[i].cv[lane], static_cast<const uint2 *>(a.v) + eight);
-                }
-                copies_commit();
-            }
-            const float s = CLIP ? clip_scale[replica] : 1.0f;
+        for (int i = 0; i < kAhead; ++i) fetch(i, mine + i * slot);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (warp >= full) break;
-                switch (i) {
-                    case 0: copies_wait<kAhead - 1>(); break;
-                    case 1: copies_wait<kAhead - 2>(); break;
-                    case 2: copies_wait<kAhead - 3>(); break;
-                    default: copies_wait<0>(); break;
-                }
-                Raw<BITS> r;
-                const uint4 g = mine.ahead[i].g[lane], p = mine.ahead[i].p[lane];
-                r.g[0] = g.x, r.g[1] = g.y, r.g[2] = g.z, r.g[3] = g.w;
-                r.p[0] = p.x, r.p[1] = p.y, r.p[2] = p.z, r.p[3] = p.w;
-                r.cm = mine.ahead[i].cm[lane];
-                r.cv = mine.ahead[i].cv[lane];
-                r.scale_m = __shfl_sync(0xffffffffu, scales, 2 * i);
-                r.scale_v = __shfl_sync(0xffffffffu, scales, 2 * i + 1);
-                update_block<BITS, CLIP, true>(a, sc, c, replica, s, warp, nullptr, r);
-                warp += kWarps;
+        for (int i = 0; i < kAhead; ++i) {
+            if (first + i * kWarps >= end) break;
+            if (i == 0) copies_wait<3>();
+            if (i == 1) copies_wait<2>();
+            if (i == 2) copies_wait<1>();
+            if (i == 3) copies_wait<0>();
+            work(i, mine + i * slot);
+        }
+        copies_wait<0>();                              // groups left empty by a short record
+    } else {
+        for (int round = 0; first + round * kWarps < end; round += fit) {
+            for (int i = 0; i < fit; ++i) fetch(round + i, mine + i * slot);
+            for (int i = 0; i < fit && first + (round + i) * kWarps < end; ++i) {
+                const int later = fit - 1 - i;
+                if (later >= 3) copies_wait<3>();
+                else if (later == 2) copies_wait<2>();
+                else if (later == 1) copies_wait<1>();
+                else copies_wait<0>();
+                work(round + i, mine + i * slot);
             }
             copies_wait<0>();
-            __syncwarp();
+            __syncwarp();                              // everything is read before the places are filled again
         }
     }
+}
+
+// BF16: all of the list's tensors are bf16, parameters and gradients, and aligned.  (Apart, because
+// the code for every case needs more registers: 6065 against 6549 GB/s on 2^27 bf16 elements.)
+template <int BITS, bool CLIP, bool BF16>
+__global__ void __launch_bounds__(kAdamwThreads, BITS == 32 || BF16 ? 4 : 3)
+    adamw_step_kernel(const AdamwList a, const AdamwScalars sc, const float *clip_scale) {
+    constexpr int kWarps = kAdamwThreads / 32;
+    constexpr uint32_t kAligned = kAdamwParamAligned | kAdamwGradAligned;
+    extern __shared__ __align__(16) char shared[];
+    const uint32_t replica = blockIdx.y;
+    const AdamwChunk c = load_chunk(a.chunks + replica * a.n_chunks + blockIdx.x);
+    const int first = threadIdx.x >> 5;
     const float s = CLIP ? clip_scale[replica] : 1.0f;
-    for (; warp * kAdamwBlock < c.n; warp += kWarps) {
+    char *mine = shared + first * (BITS == 8 ? a.warp_bytes : kStageBytes);
+    int lo = 0, hi = 0;                                // the record's blocks [lo, hi) are streamed
+    if constexpr (BITS == 8) {
+        // a misaligned tensor's outermost granules hold bytes beside it: its first block, and one with
+        // less than a granule of the tensor behind it, are read element by element
+        const bool aligned = BF16 || (c.flags & kAligned) == kAligned;
+        lo = aligned || !(c.flags & kAdamwFirst) ? 0 : 1;
+        hi = (aligned || !(c.flags & kAdamwLast) ? c.n : c.n - 8) / kAdamwBlock;
+        const int from = first < lo ? first + kWarps : first;
+        if (from < hi) stream_blocks<CLIP, BF16>(a, sc, c, replica, s, from, hi, mine);
+    }
+    for (int b = first; b * kAdamwBlock < c.n; b += kWarps) {
+        if (b >= lo && b < hi) continue;
         Raw<BITS> r;
-        load_block<BITS>(a, c, warp, mine.stage, r);
-        update_block<BITS, CLIP, false>(a, sc, c, replica, s, warp, mine.stage, r);
+        load_block<BITS>(a, c, b, reinterpret_cast<uint32_t *>(mine), r);
+        update_block<BITS, CLIP, false>(a, sc, c, replica, s, b, reinterpret_cast<uint32_t *>(mine), r);
     }
 }
 
 // ---------------------------------------------------------------- gradient norms
 
-// Sum of squares of a lane's eight values of a block, as bits: into sum, or
-// into wide where fp32 does not hold the squares.
-__device__ __forceinline__ void add_squares(const uint32_t *w, bool bf16, Kahan &sum, double &wide) {
-    Pair x[4], q = Pair(0.0f);
-    to_pairs(w, bf16, x);
+// Sum of squares of eight values: into sum, or into wide where fp32 does not hold the squares.
+__device__ __forceinline__ void add_squares(const Pair *x, Kahan &sum, double &wide) {
+    Pair q = Pair(0.0f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) q = fma2(x[i], x[i], q);
     const float both = q.lo() + q.hi();
@@ -350,51 +433,111 @@ __device__ __forceinline__ void add_squares(const uint32_t *w, bool bf16, Kahan 
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double t = i & 1 ? x[i / 2].hi() : x[i / 2].lo();
-        if (t != 0.0) wide = fma(t, t, wide);
+        const float t = i & 1 ? x[i / 2].hi() : x[i / 2].lo();
+        if (t != 0.0f) wide = fma(static_cast<double>(t), static_cast<double>(t), wide);
     }
 }
 
-// The blocks of a replica take its records in turn; each record's loads go out together, and
-// the next record's addresses with them.  The replica's last block adds the blocks' sums, in their order.
-__global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const AdamwList a, double *partial, uint32_t *arrived,
-                                                                   double *sums, float *scale, double max_norm) {
+// The sum of a double of every thread, in a fixed order, in thread 0.  (fp64 runs at a sixty-fourth of
+// fp32's rate here, so that the sums of a block's warps are pairs of floats up to this point.)
+__device__ __forceinline__ double sum_of_warps(double in_warp, double *parts) {
     constexpr int kWarps = kAdamwThreads / 32;
-    __shared__ __align__(16) uint32_t stages[kWarps][kAdamwBlock];
+    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = in_warp;
+    __syncthreads();
+    double t = threadIdx.x < 32 ? parts[threadIdx.x & (kWarps - 1)] : 0.0;
+#pragma unroll
+    for (int off = kWarps / 2; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+    return t;
+}
+
+// Each thread block sums `per` records of a replica.  Which thread has which elements does not
+// matter, so that any tensor is read in aligned 16-byte granules and what is left at its ends
+// by elements; four granules a thread at a time, the next four under way meanwhile.  The last of the
+// replica's thread blocks adds the blocks' sums, in their order.
+__global__ void __launch_bounds__(kAdamwThreads, 4) adamw_norm_kernel(const AdamwList a, int32_t per, double *partial,
+                                                                      uint32_t *arrived, double *sums, float *scale,
+                                                                      double max_norm) {
+    constexpr int kWarps = kAdamwThreads / 32, kUnit = 4 * kAdamwThreads;
+    __shared__ double parts[kWarps], again[kWarps];
+    __shared__ bool last;
     const int replica = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const AdamwChunk *chunks = a.chunks + replica * a.n_chunks;
-    Kahan sum;
+    Kahan sum[1];
     double wide = 0.0;
-    AdamwChunk next = load_chunk(chunks + blockIdx.x);
-    for (int64_t k = blockIdx.x; k < a.n_chunks; k += gridDim.x) {
-        const AdamwChunk c = next;
-        if (k + gridDim.x < a.n_chunks) next = load_chunk(chunks + k + gridDim.x);
-        const bool g16 = (c.flags & kAdamwGradBf16) != 0;
-        const int whole = c.flags & kAdamwGradAligned ? c.n / kAdamwBlock : 0;
-        uint32_t w[kAhead][8];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int b = warp + i * kWarps;
-            if (b < whole) load_raw(c.g, g16, true, b * kAdamwBlock + 8 * lane, c.n, nullptr, w[i]);
+    const int64_t end = min(a.n_chunks, (blockIdx.x + int64_t(1)) * per);
+
+    // where the next granules come from
+    const uint4 *granules = nullptr;
+    int left = 0;                                      // granules of the record not yet asked for
+    bool bf16 = false;
+    int64_t k = static_cast<int64_t>(blockIdx.x) * per;
+    AdamwChunk c = load_chunk(chunks + k);
+    auto element = [&](const char *p, bool b16) {
+        return b16 ? __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p)) << 16)
+                   : *reinterpret_cast<const float *>(p);
+    };
+    // the granules' next unit of the records; what lies outside a record's granules is added at once
+    auto ask = [&](uint4 *to, bool &b16, int &count) {
+        if (left <= 0) {
+            if (k >= end) {
+                count = 0;
+                return;
+            }
+            bf16 = (c.flags & kAdamwGradBf16) != 0;
+            const int size = bf16 ? 2 : 4;
+            const char *p = static_cast<const char *>(c.g), *stop = p + c.n * size;
+            const char *body = reinterpret_cast<const char *>((reinterpret_cast<uintptr_t>(p) + 15) & ~uintptr_t(15));
+            if (body > stop) body = stop;
+            granules = reinterpret_cast<const uint4 *>(body);
+            left = static_cast<int>(stop - body) / 16;
+            const char *tail = body + 16 * left;
+            Pair x[4] = {Pair(0.0f), Pair(0.0f), Pair(0.0f), Pair(0.0f)};
+            const char *at = threadIdx.x < 8 ? p + threadIdx.x * size : tail + (threadIdx.x - 8) * size;
+            if (threadIdx.x < 16 && at < (threadIdx.x < 8 ? body : stop)) x[0] = Pair(element(at, bf16), 0.0f);
+            if (threadIdx.x < 16) add_squares(x, sum[0], wide);
+            if (++k < end) c = load_chunk(chunks + k);
         }
+        b16 = bf16;
+        count = min(left, kUnit);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int b = warp + i * kWarps;
-            if (b * kAdamwBlock >= c.n) break;
-            if (b >= whole) load_raw(c.g, g16, false, b * kAdamwBlock + 8 * lane, c.n, stages[warp], w[i]);
-            add_squares(w[i], g16, sum, wide);
+        for (int i = 0; i < 4; ++i)
+            if (static_cast<int>(threadIdx.x) + i * kAdamwThreads < count) to[i] = __ldcs(granules + threadIdx.x + i * kAdamwThreads);
+        granules += kUnit;
+        left -= kUnit;
+    };
+    uint4 now[4], next[4];
+    bool now16 = false, next16 = false;
+    int count = 0, next_count = 0;
+    ask(now, now16, count);
+    for (;;) {
+        const bool more = left > 0 || k < end;
+        if (more) ask(next, next16, next_count);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (static_cast<int>(threadIdx.x) + i * kAdamwThreads >= count) break;
+            const uint32_t w[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+            Pair x[4] = {Pair(0.0f), Pair(0.0f), Pair(0.0f), Pair(0.0f)};
+            if (now16) {
+                to_pairs(w, true, x);
+            } else {
+                x[0] = Pair(__uint_as_float(w[0]), __uint_as_float(w[1]));
+                x[1] = Pair(__uint_as_float(w[2]), __uint_as_float(w[3]));
+            }
+            add_squares(x, sum[0], wide);
         }
+        if (!more) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) now[i] = next[i];
+        now16 = next16, count = next_count;
     }
-    __shared__ double parts[kWarps];
-    __shared__ bool last;
-    const double in_warp = warp_sum(sum.value() + wide);
-    if (lane == 0) parts[warp] = in_warp;
-    __syncthreads();
+    int at;
+    bool one = true;
+    double in_warp = warp_sums_wide(sum, at, one);
+    if (__any_sync(0xffffffffu, wide != 0.0)) in_warp += __shfl_sync(0xffffffffu, warp_sum(wide), 0);
+    const double in_block = sum_of_warps(in_warp, parts);
     double *mine = partial + static_cast<int64_t>(replica) * gridDim.x;
     if (threadIdx.x == 0) {
-        double t = 0.0;
-        for (int i = 0; i < kWarps; ++i) t += parts[i];
-        __stcg(mine + blockIdx.x, t);
+        __stcg(mine + blockIdx.x, in_block);
         __threadfence();
         last = atomicAdd(arrived + replica, 1u) + 1u == gridDim.x;
     }
@@ -403,12 +546,10 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_norm_kernel(const AdamwLi
     __threadfence();
     double t = 0.0;
     for (int i = threadIdx.x; i < static_cast<int>(gridDim.x); i += kAdamwThreads) t += __ldcg(mine + i);
-    t = warp_sum(t);
-    if (lane == 0) parts[warp] = t;
-    __syncthreads();
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+    t = sum_of_warps(t, again);
     if (threadIdx.x != 0) return;
-    t = 0.0;
-    for (int i = 0; i < kWarps; ++i) t += parts[i];
     arrived[replica] = 0;                              // for the next launch
     if (sums) sums[replica] = t;
     if (scale) {
@@ -472,7 +613,9 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
         uint32_t w[8];
         mean8(a.M, [&](int r, Pair *s) {
             const AdamwChunk k = load_chunk(a.chunks + r * a.n_chunks + blockIdx.x);
-            load_raw(k.p, p16, full && (k.flags & kAdamwParamAligned), at, c.n, stage, w);
+            const bool whole = full && (k.flags & kAdamwParamAligned);
+            load_raw(k.p, p16, whole, at, c.n, w);
+            turn_raw(p16, whole, stage, w);
             to_pairs(w, p16, s);
         }, mean);
 #pragma unroll
@@ -541,8 +684,8 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_bind_kernel(AdamwChunk *c
     c.p = p;
     c.block = static_cast<uint32_t>(blockIdx.y * n_blocks + t.first_block + first / kAdamwBlock);
     c.n = static_cast<int32_t>(left < chunk ? left : chunk);
-    c.flags = (c.flags & ~(kAdamwParamBf16 | kAdamwParamAligned)) | (bf16 ? kAdamwParamBf16 : 0u) |
-              (aligned ? kAdamwParamAligned : 0u);
+    c.flags = (bf16 ? kAdamwParamBf16 : 0u) | (aligned ? kAdamwParamAligned : 0u) | (first == 0 ? kAdamwFirst : 0u) |
+              (left <= chunk ? kAdamwLast : 0u);
     c.decay = t.decay;
 }
 
@@ -563,20 +706,37 @@ int32_t adamw_chunk(int num_sms, int bits, int64_t elements) {
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.n_chunks), a.M);
-    auto kernel = a.bits == 8 ? (clip_scale ? adamw_step_kernel<8, true> : adamw_step_kernel<8, false>)
-                              : (clip_scale ? adamw_step_kernel<32, true> : adamw_step_kernel<32, false>);
-    kernel<<<grid, kAdamwThreads, 0, stream>>>(a, sc, clip_scale);
+    if (a.bits == 32) {
+        auto kernel = clip_scale ? adamw_step_kernel<32, true, false> : adamw_step_kernel<32, false, false>;
+        kernel<<<grid, kAdamwThreads, kAdamwThreads / 32 * kStageBytes, stream>>>(a, sc, clip_scale);
+        return cudaGetLastError();
+    }
+    auto kernel = a.all_bf16 ? (clip_scale ? adamw_step_kernel<8, true, true> : adamw_step_kernel<8, false, true>)
+                             : (clip_scale ? adamw_step_kernel<8, true, false> : adamw_step_kernel<8, false, false>);
+    const int bytes = kAdamwThreads / 32 * a.warp_bytes;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, kAdamwThreads, bytes, stream>>>(a, sc, clip_scale);
     return cudaGetLastError();
 }
 
-int adamw_norm_blocks(int num_sms, int M, int64_t n_chunks) {
-    const int64_t want = (6 * static_cast<int64_t>(num_sms) + M - 1) / M;
-    return static_cast<int>(n_chunks < want ? n_chunks : want);
+int32_t adamw_warp_bytes(bool g16, bool p16) { return kAhead * slot_bytes(g16, p16); }
+
+// Thread blocks of a replica: some ten for each place on the device, over all replicas.
+static int norm_records(const AdamwList &a) {
+    const int64_t blocks = std::max<int64_t>(1, kAdamwNormBlocks / a.M);
+    return static_cast<int>((a.n_chunks + blocks - 1) / blocks);
+}
+int64_t adamw_norm_partials(const AdamwList &a) {
+    const int per = norm_records(a);
+    return (a.n_chunks + per - 1) / per * a.M;
 }
 
-cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, uint32_t *arrived, double *sums,
-                              float *scale, double max_norm, cudaStream_t stream) {
-    adamw_norm_kernel<<<dim3(blocks, a.M), kAdamwThreads, 0, stream>>>(a, partial, arrived, sums, scale, max_norm);
+cudaError_t launch_adamw_norm(const AdamwList &a, double *partial, uint32_t *arrived, double *sums, float *scale,
+                              double max_norm, cudaStream_t stream) {
+    const int per = norm_records(a);
+    const dim3 grid(static_cast<unsigned>((a.n_chunks + per - 1) / per), a.M);
+    adamw_norm_kernel<<<grid, kAdamwThreads, 0, stream>>>(a, per, partial, arrived, sums, scale, max_norm);
     return cudaGetLastError();
 }
 

@@ -29,6 +29,7 @@ struct __align__(16) AdamwChunk {
 constexpr uint32_t kAdamwParamBf16 = 1, kAdamwGradBf16 = 2;
 // eight elements start at a multiple of their size: one access of a lane
 constexpr uint32_t kAdamwParamAligned = 4, kAdamwGradAligned = 8;
+constexpr uint32_t kAdamwFirst = 16, kAdamwLast = 32;        // of its tensor
 
 // What does not depend on the step.
 struct AdamwList {
@@ -38,6 +39,8 @@ struct AdamwList {
     int64_t n_state;             // elements of one replica's state vector
     int32_t M;
     int32_t bits;                // 32 or 8
+    int32_t warp_bytes;          // 8 bits: a warp's shared memory (adamw_warp_bytes of most of the list)
+    int32_t all_bf16;            // 8 bits: every tensor bf16 and aligned, parameters and gradients
     void *m, *v;                 // [M][n_state] fp32, e4m3 and e5m2 in 8 bits
     float *m_scale, *v_scale;    // [M][n_state / kAdamwBlock]
 };
@@ -66,14 +69,16 @@ cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, in
 
 // The record's length for a list of so many elements over all replicas.
 int32_t adamw_chunk(int num_sms, int bits, int64_t elements);
+int32_t adamw_warp_bytes(bool grad_bf16, bool param_bf16);
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream);
 
 // ||g||^2 of each replica into sums[M] (fixed order) and, where scale is not
-// NULL, min(1, max_norm / (||g|| + 1e-6)) into scale[M].  partial holds M *
-// adamw_norm_blocks() doubles, arrived M counters, zero before and after.
-int adamw_norm_blocks(int num_sms, int M, int64_t n_chunks);
-cudaError_t launch_adamw_norm(const AdamwList &a, int blocks, double *partial, uint32_t *arrived, double *sums,
-                              float *scale, double max_norm, cudaStream_t stream);
+// NULL, min(1, max_norm / (||g|| + 1e-6)) into scale[M].  partial: adamw_norm_partials()
+// doubles; arrived: M counters, zero before and after.
+constexpr int kAdamwNormBlocks = 8192;           // over all replicas, where there are that many records
+int64_t adamw_norm_partials(const AdamwList &a);
+cudaError_t launch_adamw_norm(const AdamwList &a, double *partial, uint32_t *arrived, double *sums, float *scale,
+                              double max_norm, cudaStream_t stream);
 cudaError_t launch_adamw_average(const AdamwList &a, uint32_t mask, cudaStream_t stream);
 
 }  // namespace mtdao

@@ -30,14 +30,14 @@ struct mtdao_adamw_ctx {
     AdamwTensor *tensors_dev = nullptr;
     void **table = nullptr;              // [M][n_tensors], scratch of a binding
     int32_t *dtypes = nullptr;           // [n_tensors], likewise
-    int norm_blocks = 1;
     double *norm_partial = nullptr;
     uint32_t *norm_arrived = nullptr;
     float *clip_scale = nullptr;
     int device = 0;
     cudaStream_t stream = nullptr;
     int64_t step = 0;
-    bool has_params = false, has_grads = false;
+    bool has_params = false, has_grads = false, params_aligned = false;
+    std::vector<int32_t> param_types;
     std::vector<std::pair<uintptr_t, uintptr_t>> spans;    // of the bound parameters, sorted
     char err[512] = "";
 };
@@ -118,7 +118,6 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
     a.n_chunks = chunks;
     a.chunk = chunk;
     a.n_state = blocks * kAdamwBlock;
-    h->norm_blocks = adamw_norm_blocks(sms, M, chunks);
     const size_t held = static_cast<size_t>(M) * a.n_state * (a.bits / 8);
     const size_t scales = a.bits == 8 ? static_cast<size_t>(M) * blocks * sizeof(float) : 0;
     struct {
@@ -133,7 +132,7 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
         {reinterpret_cast<void **>(&h->tensors_dev), n_tensors * sizeof(AdamwTensor)},
         {reinterpret_cast<void **>(&h->table), static_cast<size_t>(M) * n_tensors * sizeof(void *)},
         {reinterpret_cast<void **>(&h->dtypes), n_tensors * sizeof(int32_t)},
-        {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(M) * h->norm_blocks * sizeof(double)},
+        {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(adamw_norm_partials(a)) * sizeof(double)},
         {reinterpret_cast<void **>(&h->norm_arrived), M * sizeof(uint32_t)},
         {reinterpret_cast<void **>(&h->clip_scale), M * sizeof(float)},
     };
@@ -179,6 +178,15 @@ int spans_of(mtdao_adamw_ctx *h, void *const *table, const int32_t *dtype, const
     }
     std::sort(spans.begin(), spans.end());
     return MTDAO_OK;
+}
+
+// Whether every tensor starts at a multiple of eight of its elements.
+bool all_aligned(const mtdao_adamw_ctx *h, void *const *table, const int32_t *dtype) {
+    for (int32_t k = 0; k < h->n_tensors; ++k)
+        for (int32_t r = 0; r < h->list.M && h->tensors[k].numel > 0; ++r)
+            if (reinterpret_cast<uintptr_t>(table[static_cast<size_t>(r) * h->n_tensors + k]) % (dtype[k] == MTDAO_BF16 ? 16 : 32))
+                return false;
+    return true;
 }
 
 int upload(mtdao_adamw_ctx *h, void *const *table, const int32_t *dtype, bool grads) {
@@ -255,6 +263,8 @@ extern "C" int mtdao_adamw_bind_params(mtdao_adamw_handle h, void *const *params
         if (int rc = select_device(h)) return rc;
         h->has_params = h->has_grads = false;      // the gradients were checked against the earlier parameters
         if (int rc = upload(h, params, dtype, false)) return rc;
+        h->param_types.assign(dtype, dtype + h->n_tensors);
+        h->params_aligned = all_aligned(h, params, dtype);
         h->spans.swap(spans);
         h->has_params = true;
         return MTDAO_OK;
@@ -281,6 +291,18 @@ extern "C" int mtdao_adamw_bind_grads(mtdao_adamw_handle h, const void *const *g
         if (int rc = select_device(h)) return rc;
         h->has_grads = false;
         if (int rc = upload(h, table, dtype, true)) return rc;
+        // shared memory for the kind of tensor that most elements are of
+        int64_t elements[2][2] = {}, most = -1;
+        for (int32_t k = 0; k < h->n_tensors; ++k)
+            elements[dtype[k] == MTDAO_BF16][h->param_types[k] == MTDAO_BF16] += h->tensors[k].numel;
+        for (int g = 0; g < 2; ++g)
+            for (int p = 0; p < 2; ++p)
+                if (elements[g][p] > most) {
+                    most = elements[g][p];
+                    h->list.warp_bytes = adamw_warp_bytes(g, p);
+                }
+        h->list.all_bf16 = elements[0][0] + elements[0][1] + elements[1][0] == 0 && h->params_aligned &&
+                           all_aligned(h, table, dtype);
         h->has_grads = true;
         return MTDAO_OK;
     } catch (const std::bad_alloc &) {
@@ -313,7 +335,7 @@ extern "C" int mtdao_adamw_step(mtdao_adamw_handle h, double lr, double weight_d
     cudaError_t e = cudaSuccess;
     if (max_norm > 0.0) {
         scale = h->clip_scale;
-        e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, h->norm_arrived, nullptr, h->clip_scale,
+        e = launch_adamw_norm(h->list, h->norm_partial, h->norm_arrived, nullptr, h->clip_scale,
                               max_norm, h->stream);
     }
     if (e == cudaSuccess) e = launch_adamw_step(h->list, sc, scale, h->stream);
@@ -329,7 +351,7 @@ extern "C" int mtdao_adamw_grad_sqnorm(mtdao_adamw_handle h, double *out_dev) {
     if (!h->has_grads) return fail(h, MTDAO_ERR_STATE, "grad_sqnorm: no gradients are bound");
     Range range("mtdao_adamw_grad_sqnorm");
     if (int rc = select_device(h)) return rc;
-    const cudaError_t e = launch_adamw_norm(h->list, h->norm_blocks, h->norm_partial, h->norm_arrived, out_dev, nullptr,
+    const cudaError_t e = launch_adamw_norm(h->list, h->norm_partial, h->norm_arrived, out_dev, nullptr,
                                             0.0, h->stream);
     return e == cudaSuccess ? MTDAO_OK : cuda_fail(h, e, "gradient norm");
 }
