@@ -22,7 +22,8 @@ INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libmtdao.so")
 SOURCES = ["mtdao_api.cu", "reduce_kernels.cu", "stats_wide.cu", "step_adam.cu", "step_adopt.cu",
-           "step_sgdm.cu", "noalloc.cu", "adamw.cu", "adamw_api.cu", "peri_norm.cu"]
+           "step_sgdm.cu", "noalloc.cu", "adamw.cu", "adamw_api.cu", "peri_norm_api.cu",
+           "peri_norm_f32.cu", "peri_norm_bf16.cu", "peri_norm_mixed.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
                      "-prec-div=true", "-prec-sqrt=true", "-ftz=false",
