@@ -299,16 +299,20 @@ __global__ void __launch_bounds__(256) peri_backward_sums_kernel(const NormArgs 
     if (kind == kGateRows && a.split) {
         const float w = valid ? a.post_w.get(c) : 0.0f, b = valid && a.post_b.p ? a.post_b.get(c) : 0.0f;
         const int64_t most = (a.rows + workers - 1) / workers;         // rows of a worker
-        for (int64_t g = 0; g < a.gate_rows; ++g) {
+        for (int64_t g = part; valid && g < a.gate_rows; g += 8) {      // gate rows over the column's threads
             const int64_t lo = g * a.per_gate / most + g, hi = ((g + 1) * a.per_gate - 1) / most + g + 1;
-            const float s = column(Ss, lo, hi), d = full ? column(Ds, lo, hi) : 0.0f;
-            if (valid) {
-                const float gate = a.gate.get(g * a.d + c);
-                post_w = fmaf(gate, s, post_w);
-                post_b = fmaf(gate, d, post_b);
-                if (part == 0) a.d_gate.set(g * a.d + c, fmaf(w, s, b * d));
+            float s = 0.0f, d = 0.0f;
+            for (int64_t k = lo; k < hi; ++k) {
+                s += Ss[k * a.d + c];
+                if (full) d += Ds[k * a.d + c];
             }
+            const float gate = a.gate.get(g * a.d + c);
+            post_w = fmaf(gate, s, post_w);
+            post_b = fmaf(gate, d, post_b);
+            a.d_gate.set(g * a.d + c, fmaf(w, s, b * d));
         }
+        post_w = reduce(post_w);
+        post_b = reduce(post_b);
     } else {
         post_w = column(Ss, 0, rows);
         post_b = full ? column(Ds, 0, rows) : 0.0f;

@@ -19,59 +19,75 @@ import paper_2510_05361_gb300 as P
 
 _CODES = {torch.float32: P.F32, torch.bfloat16: P.BF16}
 _NORMS = {"rms": P.NORM_RMS, "layer": P.NORM_LAYER}
+_stream_of = torch._C._cuda_getCurrentRawStream
+
+# A call of a few rows is bound by what happens here, so that the checks read a
+# tensor's properties once, and the C call's description of shapes (and for the
+# backward pass the size of its workspace) is kept by its contents.
+_plans = {}
+_MOST_PLANS = 4096
 
 
-def _rows(t, what, d, device):
-    """t as [rows, d], sharing its memory."""
-    if t.dtype not in _CODES:
+def _plan(key, backward):
+    plan = _plans.get(key)
+    if plan is None:
+        shape = P.mtdao_peri_norm(*key[1:])
+        plan = (shape, P.mtdao_peri_norm_workspace(shape) if backward else 0)
+        if len(_plans) >= _MOST_PLANS:
+            _plans.clear()
+        _plans[key] = plan
+    return plan
+
+
+def _rows(t, what, d, index):
+    """(t's type code, rows, elements from one row to the next)"""
+    code = _CODES.get(t.dtype)
+    if code is None:
         raise ValueError("%s: dtype %s not supported" % (what, t.dtype))
-    if t.dim() != 2:
-        if t.dim() == 0:
-            raise ValueError("%s must have rows" % what)
-        t = t.view(-1, t.shape[-1])           # raises where the rows have no common stride
-    if t.shape[1] != d:
-        raise ValueError("%s: rows of %d elements, expected %d" % (what, t.shape[1], d))
-    if t.device != device or not t.is_cuda:
+    if t.get_device() != index or index < 0:
         raise ValueError("%s must be in device memory, with the others" % what)
-    return t
-
-
-def _stride(t, what):
-    if t.shape[0] <= 1:
-        if t.shape[1] > 1 and t.numel() and t.stride(1) != 1:
-            raise ValueError("%s: rows must be contiguous" % what)
-        return t.shape[1]
-    if (t.stride(1) != 1 and t.shape[1] > 1) or t.stride(0) < t.shape[1]:
+    if t.dim() == 0 or t.shape[-1] != d:
+        raise ValueError("%s: rows of %d elements expected, got shape %s" % (what, d, tuple(t.shape)))
+    if t.is_contiguous():
+        return code, t.numel() // d if d else 0, d
+    if t.dim() != 2:
+        t = t.view(-1, d)                     # raises where the rows have no common stride
+    rows, apart = t.shape[0], t.stride(0)
+    if (t.stride(1) != 1 and d > 1) or (apart < d and rows > 1):
         raise ValueError("%s: rows must be contiguous and apart" % what)
-    return t.stride(0)
+    return code, rows, apart if rows > 1 else d
 
 
-def _vector(t, what, d, device, like=None):
-    if t is None:
-        return None
-    if t.dim() != 1 or t.shape[0] != d or not t.is_contiguous() or t.device != device:
-        raise ValueError("%s must be a contiguous vector of %d elements, with the others" % (what, d))
-    if t.dtype not in _CODES or (like is not None and t.dtype != like.dtype):
+def _vector(t, what, d, index, kind):
+    """The address of a weight or bias; kind: the weights' dtype."""
+    if t.dtype != kind or kind not in _CODES:
         raise ValueError("%s: dtype %s not supported, or not that of the other weights" % (what, t.dtype))
+    if t.dim() != 1 or t.shape[0] != d or t.get_device() != index or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d elements, with the others" % (what, d))
     return t.data_ptr()
 
 
-def _describe(rows, d, norm, stream, branch, post_weight, gate, eps, residual_scale, device):
-    """The description's leading fields, and the gate's address."""
-    if norm not in _NORMS:
+def _gate(gate, rows, d, index):
+    """(type code, gate rows, address)"""
+    if gate is None:
+        return 0, 0, None
+    code = _CODES.get(gate.dtype)
+    if code is None:
+        raise ValueError("gate: dtype %s not supported" % gate.dtype)
+    dim = gate.dim()
+    if dim not in (1, 2) or gate.shape[-1] != d or gate.get_device() != index or not gate.is_contiguous():
+        raise ValueError("gate must be contiguous, [%d] or [G, %d], with the others" % (d, d))
+    gate_rows = 1 if dim == 1 else gate.shape[0]
+    if gate_rows == 0 or rows % gate_rows:
+        raise ValueError("gate: %d rows do not divide %d" % (gate_rows, rows))
+    return code, gate_rows, gate.data_ptr()
+
+
+def _norm_code(norm):
+    code = _NORMS.get(norm)
+    if code is None:
         raise ValueError("norm must be 'rms' or 'layer'")
-    gate_rows, gate_code, gate_ptr = 0, 0, None
-    if gate is not None:
-        if gate.dim() not in (1, 2) or gate.shape[-1] != d or not gate.is_contiguous() or gate.device != device:
-            raise ValueError("gate must be contiguous, [%d] or [G, %d], with the others" % (d, d))
-        if gate.dtype not in _CODES:
-            raise ValueError("gate: dtype %s not supported" % gate.dtype)
-        gate_rows = 1 if gate.dim() == 1 else gate.shape[0]
-        if gate_rows == 0 or rows % gate_rows:
-            raise ValueError("gate: %d rows do not divide %d" % (gate_rows, rows))
-        gate_code, gate_ptr = _CODES[gate.dtype], gate.data_ptr()
-    return (rows, d, _NORMS[norm], _CODES[stream], _CODES[branch], _CODES[post_weight.dtype], gate_code,
-            gate_rows, eps, residual_scale), gate_ptr
+    return code
 
 
 def peri_norm_forward(x, f, post_weight, pre_weight, *, post_bias=None, pre_bias=None, gate=None,
@@ -80,18 +96,28 @@ def peri_norm_forward(x, f, post_weight, pre_weight, *, post_bias=None, pre_bias
     deviation) is None unless ``save``.  y has x's shape and type, h f's."""
     if x.shape != f.shape:
         raise ValueError("x and f differ in shape")
-    d, device = x.shape[-1] if x.dim() else 0, x.device
-    x2, f2 = _rows(x, "x", d, device), _rows(f, "f", d, device)
-    pw, qw = _vector(post_weight, "post_weight", d, device), _vector(pre_weight, "pre_weight", d, device, post_weight)
-    pb, qb = _vector(post_bias, "post_bias", d, device, post_weight), _vector(pre_bias, "pre_bias", d, device, post_weight)
-    head, gp = _describe(x2.shape[0], d, norm, x.dtype, f.dtype, post_weight, gate, eps, residual_scale, device)
-    y, h = torch.empty(x.shape, dtype=x.dtype, device=device), torch.empty(f.shape, dtype=f.dtype, device=device)
-    stats = torch.empty((2, x2.shape[0], 2), dtype=torch.float32, device=device) if save else None
-    shape = P.mtdao_peri_norm(*head, _stride(x2, "x"), _stride(f2, "f"), d, d, d, d, d, d)
-    with torch.cuda.device(device):
-        P.mtdao_peri_norm_forward(shape, x2.data_ptr(), f2.data_ptr(), pw, pb, qw, qb, gp, y.data_ptr(), h.data_ptr(),
-                                  None if stats is None else stats.data_ptr(),
-                                  torch.cuda.current_stream().cuda_stream)
+    index = x.get_device()
+    d = x.shape[-1] if x.dim() else 0
+    x_code, rows, ld_x = _rows(x, "x", d, index)
+    f_code, _, ld_f = _rows(f, "f", d, index)
+    kind = post_weight.dtype
+    pw, qw = _vector(post_weight, "post_weight", d, index, kind), _vector(pre_weight, "pre_weight", d, index, kind)
+    pb = None if post_bias is None else _vector(post_bias, "post_bias", d, index, kind)
+    qb = None if pre_bias is None else _vector(pre_bias, "pre_bias", d, index, kind)
+    g_code, gate_rows, gp = _gate(gate, rows, d, index)
+    shape, _ = _plan((False, rows, d, _norm_code(norm), x_code, f_code, _CODES[kind], g_code, gate_rows, eps,
+                      residual_scale, ld_x, ld_f, d, d, d, d, d, d), False)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return peri_norm_forward(x, f, post_weight, pre_weight, post_bias=post_bias, pre_bias=pre_bias, gate=gate,
+                                     residual_scale=residual_scale, eps=eps, norm=norm, save=save)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    h = torch.empty_like(f, memory_format=torch.contiguous_format)
+    stats = torch.empty((2, rows, 2), dtype=torch.float32, device=x.device) if save else None
+    rc = P.lib.mtdao_peri_norm_forward(shape, x.data_ptr(), f.data_ptr(), pw, pb, qw, qb, gp, y.data_ptr(), h.data_ptr(),
+                                       stats.data_ptr() if save else None, _stream_of(index))
+    if rc:
+        P._check(rc)
     return y, h, stats
 
 
@@ -100,39 +126,52 @@ def peri_norm_backward(dh, dy, y, f, stats, post_weight, pre_weight, *, post_bia
     """The gradients, by name: x, f, post_weight, pre_weight and, where they
     were given, post_bias, pre_bias, gate.  dh and dy are those of h and y (dy None: zero); y, f,
     stats as the forward pass had them.  A weight's gradient has its type."""
-    d, device = f.shape[-1] if f.dim() else 0, f.device
-    dh2, y2, f2 = _rows(dh, "dh", d, device), _rows(y, "y", d, device), _rows(f, "f", d, device)
-    dy2 = None if dy is None else _rows(dy, "dy", d, device)
-    rows = f2.shape[0]
-    if dh2.shape[0] != rows or y2.shape[0] != rows or (dy2 is not None and dy2.shape[0] != rows):
+    index = f.get_device()
+    d = f.shape[-1] if f.dim() else 0
+    f_code, rows, ld_f = _rows(f, "f", d, index)
+    h_code, h_rows, ld_dh = _rows(dh, "dh", d, index)
+    y_code, y_rows, ld_y = _rows(y, "y", d, index)
+    dy_code, dy_rows, ld_dy = (y_code, rows, d) if dy is None else _rows(dy, "dy", d, index)
+    if h_rows != rows or y_rows != rows or dy_rows != rows:
         raise ValueError("dh, dy, y and f differ in shape")
-    if dh.dtype != f.dtype or (dy is not None and dy.dtype != y.dtype):
+    if h_code != f_code or dy_code != y_code:
         raise ValueError("dh must have f's dtype, dy that of y")
-    if stats.shape != (2, rows, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != device:
+    if (stats.shape != (2, rows, 2) or stats.dtype != torch.float32 or stats.get_device() != index
+            or not stats.is_contiguous()):
         raise ValueError("stats must be what the forward pass gave: [2, %d, 2] fp32" % rows)
-    pw, qw = _vector(post_weight, "post_weight", d, device), _vector(pre_weight, "pre_weight", d, device, post_weight)
-    pb = _vector(post_bias, "post_bias", d, device, post_weight)
+    kind = post_weight.dtype
+    pw, qw = _vector(post_weight, "post_weight", d, index, kind), _vector(pre_weight, "pre_weight", d, index, kind)
     if (post_bias is None) != (pre_bias is None):
         raise ValueError("post_bias and pre_bias come together")
-    _vector(pre_bias, "pre_bias", d, device, post_weight)
-    head, gp = _describe(rows, d, norm, y.dtype, f.dtype, post_weight, gate, 0.0, residual_scale, device)
-    shape = P.mtdao_peri_norm(*head, d, _stride(f2, "f"), _stride(y2, "y"), d,
-                              d if dy2 is None else _stride(dy2, "dy"), _stride(dh2, "dh"), d, d)
-    out = {"x": torch.empty(y.shape, dtype=y.dtype, device=device),
-           "f": torch.empty(f.shape, dtype=f.dtype, device=device),
-           "post_weight": torch.empty_like(post_weight), "pre_weight": torch.empty_like(pre_weight)}
+    pb = None
     if post_bias is not None:
-        out["post_bias"], out["pre_bias"] = torch.empty_like(post_bias), torch.empty_like(pre_bias)
-    if gate is not None:
-        out["gate"] = torch.empty_like(gate)
-    at = lambda name: out[name].data_ptr() if name in out else None  # noqa: E731
-    with torch.cuda.device(device):
-        need = P.mtdao_peri_norm_workspace(shape)
-        work = torch.empty((need,), dtype=torch.uint8, device=device)
-        P.mtdao_peri_norm_backward(shape, dh2.data_ptr(), None if dy2 is None else dy2.data_ptr(), y2.data_ptr(),
-                                   f2.data_ptr(), stats.data_ptr(), pw, pb, qw, gp, at("x"), at("f"),
-                                   at("post_weight"), at("post_bias"), at("pre_weight"), at("pre_bias"), at("gate"),
-                                   work.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+        pb = _vector(post_bias, "post_bias", d, index, kind)
+        _vector(pre_bias, "pre_bias", d, index, kind)
+    g_code, gate_rows, gp = _gate(gate, rows, d, index)
+    shape, need = _plan((True, rows, d, _norm_code(norm), y_code, f_code, _CODES[kind], g_code, gate_rows, 0.0,
+                         residual_scale, d, ld_f, ld_y, d, ld_dy, ld_dh, d, d), True)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return peri_norm_backward(dh, dy, y, f, stats, post_weight, pre_weight, post_bias=post_bias, pre_bias=pre_bias,
+                                      gate=gate, residual_scale=residual_scale, norm=norm)
+    dx = torch.empty_like(y, memory_format=torch.contiguous_format)
+    df = torch.empty_like(f, memory_format=torch.contiguous_format)
+    d_pw, d_qw = torch.empty_like(post_weight), torch.empty_like(pre_weight)
+    out = {"x": dx, "f": df, "post_weight": d_pw, "pre_weight": d_qw}
+    d_pb = d_qb = dg = None
+    if pb is not None:
+        out["post_bias"], out["pre_bias"] = d_pb, d_qb = torch.empty_like(post_bias), torch.empty_like(pre_bias)
+        d_pb, d_qb = d_pb.data_ptr(), d_qb.data_ptr()
+    if gp is not None:
+        out["gate"] = dg = torch.empty_like(gate)
+        dg = dg.data_ptr()
+    work = torch.empty((need,), dtype=torch.uint8, device=f.device)
+    rc = P.lib.mtdao_peri_norm_backward(shape, dh.data_ptr(), None if dy is None else dy.data_ptr(), y.data_ptr(),
+                                        f.data_ptr(), stats.data_ptr(), pw, pb, qw, gp, dx.data_ptr(), df.data_ptr(),
+                                        d_pw.data_ptr(), d_pb, d_qw.data_ptr(), d_qb, dg, work.data_ptr(), need,
+                                        _stream_of(index))
+    if rc:
+        P._check(rc)
     return out
 
 
