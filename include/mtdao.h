@@ -575,9 +575,9 @@ int mtdao_adamw_grad_sqnorm(mtdao_adamw_handle h, double *out_dev);
 
 /*
  * Replace on every replica the masked quantities (bit 0: parameters, 1: m,
- * 2: v) by their mean over the replicas, formed in fp32 as s_0 plus the mean
- * of the differences to s_0.  Equal replicas stay as they are, but for a v
- * code that its block's scale can hold better.
+ * 2: v) by their mean over the replicas: fp32 values as s_0 plus the mean of
+ * the differences to s_0 (as mtdao_sync), bf16 values and codes as their fp32 sum divided by M, which is exact but for
+ * values of very different size.  Equal replicas stay as they are.
  */
 int mtdao_adamw_average(mtdao_adamw_handle h, uint32_t mask);
 

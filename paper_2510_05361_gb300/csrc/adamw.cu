@@ -595,14 +595,10 @@ __device__ __forceinline__ void mean8(int M, Get get, Pair *out) {
     for (int i = 0; i < 4; ++i) out[i] = Pair(mean[2 * i], mean[2 * i + 1]);
 }
 
+// One block of a record, averaged over the replicas: what is read element by element, and 32-bit states.
 template <int BITS>
-__global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const AdamwList a, uint32_t mask) {
-    __shared__ __align__(16) uint32_t stages[kAdamwThreads / 32][kAdamwBlock];
-    const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);
-    const int lane = threadIdx.x & 31;
-    for (int warp = threadIdx.x >> 5; warp * kAdamwBlock < c.n; warp += kAdamwThreads / 32) {
-    uint32_t *stage = stages[threadIdx.x >> 5];
-    const int at = warp * kAdamwBlock + 8 * lane;
+__device__ __forceinline__ void average_block(const AdamwList &a, const AdamwChunk &c, uint32_t mask, int warp, uint32_t *stage) {
+    const int lane = threadIdx.x & 31, at = warp * kAdamwBlock + 8 * lane;
     const int64_t blocks = a.n_state / kAdamwBlock;
     const int64_t block = c.block + warp;
     const int64_t e = block * kAdamwBlock + 8 * lane;
@@ -652,7 +648,177 @@ __global__ void __launch_bounds__(kAdamwThreads) adamw_average_kernel(const Adam
             for (int r = 0; r < a.M; ++r) store_pairs(s32 + r * a.n_state + e, mean);
         }
     }
+}
+
+// A replica's block on its way: parameters, codes and scales.
+__host__ __device__ __forceinline__ int replica_bytes(bool p16) { return tensor_bytes(p16) + 2 * 256 + 16; }
+constexpr int kBatch = 2, kBatches = 4;                // replicas asked for together, and how many such batches at once
+
+// 8 bits.  A warp's blocks of a record, each over the replicas in batches; the next batch, of this block or the next, is on
+// its way meanwhile.  Sums of codes times powers of two, and of bf16 values, are all but exact in fp32: they are
+// formed as they are; fp32 parameters (not P16) as in replica_mean.cuh.
+template <bool P16>
+__device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwChunk &c, uint32_t mask, int first, int end, char *mine) {
+    constexpr int kWarps = kAdamwThreads / 32;
+    const int lane = threadIdx.x & 31, M = a.M;
+    constexpr bool p16 = P16;
+    const int64_t blocks = a.n_state / kAdamwBlock;
+    const int codes_at = tensor_bytes(p16), scales_at = codes_at + 512, slot = replica_bytes(p16);
+    const int batches = (M + kBatch - 1) / kBatch, items = ((end - first + kWarps - 1) / kWarps) * batches;
+    // lane l keeps the address of replica l's parameters, the first 32 of them
+    const char *own = nullptr;
+    if (lane < M) own = static_cast<const char *>(load_chunk(a.chunks + lane * a.n_chunks + blockIdx.x).p);
+    auto params_of = [&](int r) {
+        return r < 32 ? reinterpret_cast<const char *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), r))
+                      : static_cast<const char *>(load_chunk(a.chunks + r * a.n_chunks + blockIdx.x).p);
+    };
+    int ask_block = first, ask_batch = 0, asked = 0;
+    auto fetch = [&]() {
+        if (asked < items) {
+            char *to = mine + asked % kBatches * kBatch * slot;
+            const int64_t block = c.block + ask_block;
+            for (int k = 0; k < kBatch && ask_batch * kBatch + k < M; ++k, to += slot) {
+                const int r = ask_batch * kBatch + k;
+                if (mask & 1u) {
+                    const char *p = params_of(r) + ask_block * (p16 ? 512 : 1024);
+                    copy_elements(to, p, p16, static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15));
+                }
+                const int64_t eight = (r * blocks + block) * (kAdamwBlock / 8) + lane;
+                if (mask & 2u) copy_async<8>(to + codes_at + 8 * lane, static_cast<const uint2 *>(a.m) + eight);
+                if (mask & 4u) copy_async<8>(to + codes_at + 256 + 8 * lane, static_cast<const uint2 *>(a.v) + eight);
+                if (lane < 2) copy_async<4>(to + scales_at + 4 * lane, (lane ? a.v_scale : a.m_scale) + r * blocks + block);
+            }
+            if (++ask_batch == batches) ask_batch = 0, ask_block += kWarps;
+            ++asked;
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kBatches; ++i) fetch();
+    int done = 0;
+    for (int b = first; b < end; b += kWarps) {
+        Pair ps[4], ms[4], vs[4];
+        DiffSum pd[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ps[i] = ms[i] = vs[i] = Pair(0.0f);
+        for (int batch = 0; batch < batches; ++batch, ++done) {
+            copies_wait<kBatches - 1>();
+            __syncwarp();
+            const char *at = mine + done % kBatches * kBatch * slot;
+            for (int k = 0; k < kBatch && batch * kBatch + k < M; ++k, at += slot) {
+                const int r = batch * kBatch + k;
+                if (mask & 1u) {
+                    uint32_t w[8];
+                    Pair p[4];
+                    read_elements(at, p16, static_cast<int>(reinterpret_cast<uintptr_t>(params_of(r)) & 15), w);
+                    to_pairs(w, p16, p);
+                    if (p16) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) ps[i] = ps[i] + p[i];
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float x = i & 1 ? p[i / 2].hi() : p[i / 2].lo();
+                            if (r == 0) pd[i] = DiffSum(x); else pd[i].add(x);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) ps[i] = ps[i] + p[i];      // for what is not finite
+                    }
+                }
+                const float2 scale = *reinterpret_cast<const float2 *>(at + scales_at);
+                Pair t[4];
+                if (mask & 2u) {
+                    decode_m(reinterpret_cast<const uint2 *>(at + codes_at)[lane], scale.x, t);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ms[i] = ms[i] + t[i];
+                }
+                if (mask & 4u) {
+                    decode_v(reinterpret_cast<const uint2 *>(at + codes_at + 256)[lane], scale.y, t);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vs[i] = vs[i] + t[i];
+                }
+            }
+            __syncwarp();                              // everything is read before the place is filled again
+            fetch();
+        }
+        const float count = static_cast<float>(M), part = 1.0f / count;
+        const bool exact = (M & (M - 1)) == 0;         // then the product is the quotient
+        auto mean = [&](Pair x) { return exact ? x * Pair(part) : Pair(x.lo() / count, x.hi() / count); };
+        const int64_t block = c.block + b;
+        uint32_t w[8];
+        uint2 cm = {}, cv = {};
+        float scale_m = 0.0f, scale_v = 0.0f;
+        if (mask & 1u) {
+            if (p16) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Pair x = mean(ps[i]);
+                    w[i] = bf16_nearest2(x.lo(), x.hi());
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float q = pd[i].partial() / count;
+                    w[i] = __float_as_uint(mean_or_plain(q == 0.0f ? pd[i].s0 : pd[i].s0 + q, i & 1 ? ps[i / 2].hi() : ps[i / 2].lo(), count));
+                }
+            }
+        }
+        if (mask & 2u) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ms[i] = mean(ms[i]);
+            cm = encode_m<false>(ms, 0, scale_m);
+        }
+        if (mask & 4u) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vs[i] = mean(vs[i]);
+            cv = encode_v<false>(vs, 0, scale_v);
+        }
+        for (int r = 0; r < M; ++r) {
+            const int64_t eight = (r * blocks + block) * (kAdamwBlock / 8) + lane;
+            if (mask & 1u) {
+                char *p = const_cast<char *>(params_of(r));
+                const bool whole = reinterpret_cast<uintptr_t>(p) % (p16 ? 16 : 32) == 0;
+                store_raw(p, p16, whole, b * kAdamwBlock + 8 * lane, c.n, reinterpret_cast<uint32_t *>(mine + kBatches * kBatch * slot), w);
+            }
+            if (mask & 2u) {
+                __stcs(static_cast<uint2 *>(a.m) + eight, cm);
+                if (lane == 0) a.m_scale[r * blocks + block] = scale_m;
+            }
+            if (mask & 4u) {
+                __stcs(static_cast<uint2 *>(a.v) + eight, cv);
+                if (lane == 0) a.v_scale[r * blocks + block] = scale_v;
+            }
+        }
     }
+    copies_wait<0>();
+    __syncwarp();
+}
+__host__ __device__ __forceinline__ int average_warp_bytes(bool p16) { return kBatches * kBatch * replica_bytes(p16) + kStageBytes; }
+
+// P16: the list's parameters are mostly bf16; records of the other type are averaged block by block.
+template <int BITS, bool P16>
+__global__ void __launch_bounds__(kAdamwThreads, BITS == 32 ? 4 : P16 ? 3 : 2) adamw_average_kernel(const AdamwList a, uint32_t mask, int warp_bytes) {
+    constexpr int kWarps = kAdamwThreads / 32;
+    extern __shared__ __align__(16) char shared[];
+    const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);
+    const int first = threadIdx.x >> 5;
+    char *mine = shared + first * warp_bytes;
+    int lo = 0, hi = 0;
+    if constexpr (BITS == 8) {
+        // as in the step: no granule that holds bytes beside the tensor (any replica's may be misaligned)
+        const bool first_record = c.flags & kAdamwFirst, last_record = c.flags & kAdamwLast;
+        bool aligned = true;
+        for (int r = threadIdx.x & 31; r < a.M; r += 32)
+            aligned &= (load_chunk(a.chunks + r * a.n_chunks + blockIdx.x).flags & kAdamwParamAligned) != 0;
+        aligned = __all_sync(0xffffffffu, aligned);
+        lo = aligned || !first_record ? 0 : 1;
+        hi = (aligned || !last_record ? c.n : c.n - 8) / kAdamwBlock;
+        if (((c.flags & kAdamwParamBf16) != 0) != P16) hi = lo = 0;
+        const int from = first < lo ? first + kWarps : first;
+        if (from < hi) average_stream<P16>(a, c, mask, from, hi, mine);
+    }
+    for (int b = first; b * kAdamwBlock < c.n; b += kWarps)
+        if (b < lo || b >= hi) average_block<BITS>(a, c, mask, b, reinterpret_cast<uint32_t *>(mine));
 }
 
 // ---------------------------------------------------------------- records
@@ -742,10 +908,15 @@ cudaError_t launch_adamw_norm(const AdamwList &a, double *partial, uint32_t *arr
 
 cudaError_t launch_adamw_average(const AdamwList &a, uint32_t mask, cudaStream_t stream) {
     const unsigned grid = static_cast<unsigned>(a.n_chunks);
-    if (a.bits == 8)
-        adamw_average_kernel<8><<<grid, kAdamwThreads, 0, stream>>>(a, mask);
-    else
-        adamw_average_kernel<32><<<grid, kAdamwThreads, 0, stream>>>(a, mask);
+    if (a.bits == 32) {
+        adamw_average_kernel<32, false><<<grid, kAdamwThreads, kAdamwThreads / 32 * kStageBytes, stream>>>(a, mask, kStageBytes);
+        return cudaGetLastError();
+    }
+    auto kernel = a.params_bf16 ? adamw_average_kernel<8, true> : adamw_average_kernel<8, false>;
+    const int warp_bytes = average_warp_bytes(a.params_bf16), bytes = kAdamwThreads / 32 * warp_bytes;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, kAdamwThreads, bytes, stream>>>(a, mask, warp_bytes);
     return cudaGetLastError();
 }
 

@@ -40,6 +40,7 @@ struct AdamwList {
     int32_t M;
     int32_t bits;                // 32 or 8
     int32_t warp_bytes;          // 8 bits: a warp's shared memory (adamw_warp_bytes of most of the list)
+    int32_t params_bf16;         // 8 bits: most parameters are
     int32_t all_bf16;            // 8 bits: every tensor bf16 and aligned, parameters and gradients
     void *m, *v;                 // [M][n_state] fp32, e4m3 and e5m2 in 8 bits
     float *m_scale, *v_scale;    // [M][n_state / kAdamwBlock]

@@ -265,6 +265,12 @@ extern "C" int mtdao_adamw_bind_params(mtdao_adamw_handle h, void *const *params
         if (int rc = upload(h, params, dtype, false)) return rc;
         h->param_types.assign(dtype, dtype + h->n_tensors);
         h->params_aligned = all_aligned(h, params, dtype);
+        int64_t bf16 = 0, all = 0;
+        for (int32_t k = 0; k < h->n_tensors; ++k) {
+            all += h->tensors[k].numel;
+            if (dtype[k] == MTDAO_BF16) bf16 += h->tensors[k].numel;
+        }
+        h->list.params_bf16 = 2 * bf16 > all;
         h->spans.swap(spans);
         h->has_params = true;
         return MTDAO_OK;
