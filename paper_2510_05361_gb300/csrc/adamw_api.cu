@@ -63,6 +63,7 @@ int fail(mtdao_adamw_ctx *h, int code, const char *fmt, ...) {
     return code;
 }
 int cuda_fail(mtdao_adamw_ctx *h, cudaError_t e, const char *what) {
+    cudaGetLastError();                                // reported here, not by the next launch
     return fail(h, MTDAO_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "pair.cuh"
+
 namespace mtdao {
 
 __host__ __device__ __forceinline__ uint64_t splitmix64(uint64_t z) {
@@ -32,38 +34,6 @@ struct CodeM {
 struct CodeV {
     static constexpr int kTop = 14, kDrop = 21;
 };
-
-// Two fp32 operations in one instruction, each rounded as the single ones are.
-struct Pair {
-    uint64_t bits;
-    __device__ __forceinline__ Pair() {}
-    __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(lo), "f"(hi)); }
-    __device__ __forceinline__ explicit Pair(float both) : Pair(both, both) {}
-    __device__ __forceinline__ void get(float &lo, float &hi) const {
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(bits));
-    }
-    __device__ __forceinline__ float lo() const { float a, b; get(a, b); return a; }
-    __device__ __forceinline__ float hi() const { float a, b; get(a, b); return b; }
-};
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
-    return r;
-}
-__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
-    return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
-    return r;
-}
-
-// a b, rounded, also where it is added to something next: the assembler fuses a packed
-// product and sum (seen in a result's last bit), but not this.
-__device__ __forceinline__ Pair product(Pair a, Pair b) { return fma2(a, b, Pair(0.0f)); }
 
 // The scale of a block of a given largest magnitude, and its inverse: powers of two, so that
 // scaling rounds nothing.

@@ -7,6 +7,7 @@
 
 #include "mtdao.h"
 #include "mtdao_internal.h"
+#include "pair.cuh"
 
 namespace mtdao {
 
@@ -31,6 +32,15 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     return r;
 }
 
+// Copies to shared memory that run while the thread goes on.
+__device__ __forceinline__ void copy_async16(void *to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                 :: "r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(LATER) : "memory"); }
+
 // Eight elements of a row as they lie in memory: one access of 16 (bf16) or 32 bytes (fp32).
 template <typename T>
 struct Eight;
@@ -40,11 +50,18 @@ struct Eight<Bf16> {
     __device__ __forceinline__ float get(int i) const {
         return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
+    __device__ __forceinline__ Pair pair(int i) const {
+        return Pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
     __device__ __forceinline__ void set(const float *x) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = bf16x2(x[2 * i], x[2 * i + 1]);
     }
     __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ void from_shared(const char *at, int apart) {      // pieces of 16 bytes
+        const uint4 q = *reinterpret_cast<const uint4 *>(at);
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    }
     __device__ __forceinline__ void put(int i, Bf16 x) {
         w[i / 2] |= static_cast<uint32_t>(x.bits) << (16 * (i & 1));
     }
@@ -64,6 +81,7 @@ template <>
 struct Eight<float> {
     float w[8];
     __device__ __forceinline__ float get(int i) const { return w[i]; }
+    __device__ __forceinline__ Pair pair(int i) const { return Pair(w[2 * i], w[2 * i + 1]); }
     __device__ __forceinline__ void set(const float *x) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = x[i];
@@ -73,6 +91,10 @@ struct Eight<float> {
         for (int i = 0; i < 8; ++i) w[i] = 0.0f;
     }
     __device__ __forceinline__ void put(int i, float x) { w[i] = x; }
+    __device__ __forceinline__ void from_shared(const char *at, int apart) {
+        const float4 a = *reinterpret_cast<const float4 *>(at), b = *reinterpret_cast<const float4 *>(at + apart);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
     __device__ __forceinline__ void load(const float *p) {
         asm volatile("ld.global.cs.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]), "=f"(w[4]), "=f"(w[5]), "=f"(w[6]), "=f"(w[7])
@@ -111,6 +133,13 @@ struct Columns {
         }
     }
     template <typename T>
+    __device__ __forceinline__ void store(T *row, int q, const Pair *x) const {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].get(y[2 * i], y[2 * i + 1]);
+        store(row, q, y);
+    }
+    template <typename T>
     __device__ __forceinline__ void store(T *row, int q, const float *x) const {
         if constexpr (VEC) {
             Eight<T> e;
@@ -135,6 +164,13 @@ struct Vector {
     __device__ __forceinline__ void set(int64_t i, float x) const {
         if (bf16) static_cast<Bf16 *>(p)[i] = rounded<Bf16>(x);
         else static_cast<float *>(p)[i] = x;
+    }
+    template <bool VEC>
+    __device__ __forceinline__ void load(const Columns<VEC> &c, int64_t row, int q, Pair *x) const {
+        float y[8];
+        load(c, row, q, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = Pair(y[2 * i], y[2 * i + 1]);
     }
     template <bool VEC>
     __device__ __forceinline__ void load(const Columns<VEC> &c, int64_t row, int q, float *x) const {
@@ -194,11 +230,13 @@ cudaError_t launch_peri_backward(const NormArgs &a, bool vec, cudaStream_t strea
 
 // Workspace of the backward pass, in floats, and how its rows are dealt out.
 struct BackwardPlan {
+    int groups_of_eight;                    // columns of a thread
+    int lanes;                              // of a row, where it has one warp or less
     int warps;                              // of a row, in one thread block
     int cluster;                            // thread blocks of a row
     int groups;                             // rows that a thread block works on at a time
     int64_t blocks;                         // thread blocks, or clusters of them
-    bool contiguous, split;
+    bool contiguous, split, full;
     int64_t floats;
 };
 constexpr int kPeriSms = 152;               // of the device that this is written for: sizes grids, no more

@@ -13,17 +13,31 @@
 
 namespace mtdao {
 
-// Warps of a row: each thread has eight columns; more than 16 warps are spread over a cluster of thread blocks.
-// About two thread blocks of eight warps an SM; fewer where rows run out.
+// A thread has sixteen columns of a row where it keeps two sums for each, else eight (four sums of sixteen are more than
+// its registers hold); rows too long for one thread block are spread over a cluster of them.  512 threads an
+// SM; fewer where rows run out.
 BackwardPlan plan_backward(const NormArgs &a, bool vec) {
     BackwardPlan p = {};
-    const int need = (a.d + 255) / 256;
-    p.cluster = need <= 16 ? 1 : vec && need <= 32 ? 2 : 4;
-    if (need > 16) p.warps = 16;
-    else if (!vec) p.warps = need <= 1 ? 1 : need <= 4 ? 4 : 16;
-    else p.warps = need <= 4 ? need : need <= 8 ? 8 : 16;
-    p.groups = p.warps <= 1 ? 8 : p.warps == 2 ? 4 : p.warps <= 4 ? 2 : 1;
-    const int64_t most = 2 * kPeriSms / (p.cluster * std::max(1, p.warps / 8));
+    p.full = a.layer || a.post_b.p || !vec;            // rows of odd columns have one kernel for both
+    p.cluster = p.warps = p.groups_of_eight = 1;
+    p.lanes = 32;
+    if (!vec) {
+        p.warps = a.d <= 256 ? 1 : a.d <= 1024 ? 4 : 16;
+        p.cluster = a.d <= 4096 ? 1 : 4;
+    } else if (a.d <= 256) {
+        p.lanes = a.d <= 64 ? 8 : a.d <= 128 ? 16 : 32;
+    } else if (p.full) {
+        const int need = (a.d + 255) / 256;
+        p.warps = need <= 4 ? need : need <= 8 ? 8 : 16;
+        while (4096 * p.cluster < a.d) p.cluster *= 2;
+    } else {
+        p.groups_of_eight = 2;
+        while (512 * p.warps < a.d && p.warps < 8) p.warps *= 2;
+        while (4096 * p.cluster < a.d) p.cluster *= 2;
+    }
+    const int threads = p.warps == 3 ? 96 : p.warps <= 4 ? 128 : 32 * p.warps;
+    p.groups = threads / (p.warps == 1 ? p.lanes : 32 * p.warps);
+    const int64_t most = kPeriSms * (512 / threads) / p.cluster;
     p.blocks = std::max<int64_t>(1, std::min(most, (a.rows + p.groups - 1) / p.groups));
     const int64_t workers = p.blocks * p.groups;
     const bool rows_gate = gate_kind(a) == kGateRows;
@@ -90,7 +104,6 @@ NormArgs arguments(const mtdao_peri_norm *s) {
     a.eps = static_cast<float>(s->eps);
     a.residual_scale = static_cast<float>(s->residual_scale);
     a.ld_x = s->ld_x, a.ld_f = s->ld_f, a.ld_y = s->ld_y, a.ld_h = s->ld_h;
-    a.gate.p = s->gate_rows > 0 ? const_cast<mtdao_peri_norm *>(s) : nullptr;      // the plan asks whether there is one
     a.ld_dy = s->ld_dy, a.ld_dh = s->ld_dh, a.ld_dx = s->ld_dx, a.ld_df = s->ld_df;
     return a;
 }
@@ -99,6 +112,7 @@ Vector vector_of(const void *p, int32_t type) { return Vector{const_cast<void *>
 
 int done(cudaError_t e, const char *what) {
     if (e == cudaSuccess) return MTDAO_OK;
+    cudaGetLastError();                                // reported here, not by the next launch
     char msg[256];
     snprintf(msg, sizeof msg, "%s: %s", what, cudaGetErrorString(e));
     return set_thread_error(MTDAO_ERR_CUDA, msg);
@@ -144,8 +158,16 @@ extern "C" int mtdao_peri_norm_forward(const mtdao_peri_norm *s, const void *x, 
 
 extern "C" int64_t mtdao_peri_norm_workspace(const mtdao_peri_norm *s) {
     if (check_shape(s, true)) return -1;
-    const NormArgs a = arguments(s);
-    return std::max(plan_backward(a, true).floats, plan_backward(a, false).floats) * static_cast<int64_t>(sizeof(float));
+    // whatever the addresses and the biases turn out to be: the most that a plan can need
+    NormArgs a = arguments(s);
+    a.gate.p = s->gate_rows > 0 ? const_cast<mtdao_peri_norm *>(s) : nullptr;      // any address: there is a gate
+    int64_t floats = plan_backward(a, false).floats;
+    if (s->d % 8 == 0) {
+        floats = std::max(floats, plan_backward(a, true).floats);
+        a.post_b.p = const_cast<mtdao_peri_norm *>(s);
+        floats = std::max(floats, plan_backward(a, true).floats);
+    }
+    return floats * static_cast<int64_t>(sizeof(float));
 }
 
 extern "C" int mtdao_peri_norm_backward(const mtdao_peri_norm *s, const void *dh, const void *dy, const void *y,

@@ -1,9 +1,10 @@
 // peri_norm_backward.cuh -- the gradients of the Peri-LN residual update (formulas in mtdao.h).
 //
-// One pass over the rows.  A thread has the same eight columns of every row that its worker takes (a
-// worker: the warps of one row, in one thread block or a cluster of them), so that the sums over rows which
+// One pass over the rows.  A thread has the same eight or sixteen columns of every row that its worker takes (a
+// worker: the lanes or warps of one row, in one thread block or a cluster of them), so that the sums over rows which
 // the weights' gradients are stay in its registers; a row's own two sums (of the norm before the
-// block, then of the one after it) go over the worker's warps.  The next row is on its way while one is worked on.
+// block, then of the one after it) go over the worker's warps.  The next row is on its way to
+// shared memory while one is worked on; a thread reads only what it copied itself.
 // Four sums a column: of dh n_y, dh, dY n_f, dY, from which a gate that is the
 // same for the rows summed gives its own gradient and the norm's (post_w S is the gate's, gate S the weight's).
 //
@@ -16,19 +17,14 @@
 
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "peri_norm.cuh"
 
 namespace mtdao {
 namespace {
 
-template <typename S, typename B>
-struct BackRow {
-    Eight<S> y, dy;
-    Eight<B> dh, f;
-    float2 sf, sy;
-};
-
-template <int W, int G, int C>
+template <int W, int L, int G, int C>
 struct RowSums {
     float parts[G][2][2][W * C];                       // worker's row, use, value
     static constexpr int kWarps = W * C;
@@ -39,7 +35,7 @@ struct RowSums {
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) v[n] += __shfl_xor_sync(0xffffffffu, v[n], off);
+            for (int off = L / 2; off > 0; off >>= 1) v[n] += __shfl_xor_sync(0xffffffffu, v[n], off);
         if constexpr (kWarps > 1) {
             const int lane = threadIdx.x & 31, group = threadIdx.x / (32 * W), warp = threadIdx.x / 32 % W;
             if constexpr (C > 1) {
@@ -78,48 +74,94 @@ struct RowSums {
     }
 };
 
-// FULL: "layer" norm or biases; else the sums of dh and dY and the means are left out.
-template <typename S, typename B, int W, int G, int C, bool VEC, bool FULL>
-__global__ void __launch_bounds__(32 * W * G, W == 16 ? 1 : 2) peri_backward_kernel(const NormArgs a) {
+// Thread blocks of 128 threads, or 256 of a longer row; 512 threads an SM.
+template <int W>
+constexpr int kBackThreads = W == 3 ? 96 : W <= 4 ? 128 : 32 * W;
+
+// V groups of eight columns a thread.  FULL: "layer" norm or biases; else the sums of dh and dY and the means are
+// left out.
+template <typename S, typename B, int V, int W, int L, int C, bool VEC, bool FULL>
+__global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_backward_kernel(const NormArgs a) {
     constexpr int kSums = FULL ? 4 : 2;                 // A, S or A, S, B, D
-    __shared__ RowSums<W, G, C> sums;
-    __shared__ float joined[G > 1 ? 32 * W * G * 8 : 1];
-    const int group = threadIdx.x / (32 * W);
+    constexpr int kBlock = kBackThreads<W>, kThreads = W == 1 ? L : 32 * W, G = kBlock / kThreads;
+    constexpr int kPieces = 2 * (static_cast<int>(sizeof(S)) + static_cast<int>(sizeof(B))) / 2;     // of 16 bytes, of a group of columns
+    constexpr int kAhead = 2;
+    extern __shared__ __align__(16) char incoming[];    // [kAhead][V][kPieces][threads][16]
+    __shared__ RowSums<W, L, G, C> sums;
+    const int group = threadIdx.x / kThreads;
     const int rank = C > 1 ? static_cast<int>(cooperative_groups::this_cluster().block_rank()) : 0;
     const int64_t block = blockIdx.x / C, worker = block * G + group, workers = static_cast<int64_t>(gridDim.x / C) * G;
-    const Columns<VEC> cols{rank * 32 * W + static_cast<int>(threadIdx.x) % (32 * W), 32 * W * C, a.d};
+    const Columns<VEC> cols{rank * kThreads + static_cast<int>(threadIdx.x) % kThreads, kThreads * C, a.d};
     const float inv_d = 1.0f / static_cast<float>(a.d);
     const int kind = gate_kind(a);
 
-    int64_t r = worker, end = a.rows, step = workers;
+    // a worker's rows: first, first + step, ... below end.  The workers of one warp go through as many rounds.
+    int64_t first = worker, end = a.rows, step = workers, rounds = (a.rows - block * G + workers - 1) / workers;
     if (a.contiguous) {
         const int64_t unit = a.split ? 1 : a.per_gate, units = a.rows / unit, most = (units + workers - 1) / workers;
-        r = min(units, worker * most) * unit;
+        first = min(units, worker * most) * unit;
         end = min(units, (worker + 1) * most) * unit;
         step = 1;
+        rounds = min(units - min(units, block * G * most), most) * unit;
     }
-    float pre_w[8], through[8], sum[kSums][8];           // through: post_w times the gate of the rows
-    a.pre_w.load(cols, 0, 0, pre_w);
+    Pair pre_w[V][4], through[V][4], sum[kSums][V][4];   // through: post_w times the gate of the rows
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int q = 0; q < V; ++q) {
+        a.pre_w.load(cols, 0, q, pre_w[q]);
 #pragma unroll
-        for (int k = 0; k < kSums; ++k) sum[k][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int k = 0; k < kSums; ++k) sum[k][q][i] = Pair(0.0f);
+        }
     }
+    auto at = [](const Pair *x, int i) { return i & 1 ? x[i / 2].hi() : x[i / 2].lo(); };
     auto set_gate = [&](int64_t row) {
-        a.post_w.load(cols, 0, 0, through);
-        if (kind == kGateNone || kind == kGateElement) return;
-        float g[8];
-        a.gate.load(cols, gate_row(a, row), 0, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) through[i] *= g[i];
+        for (int q = 0; q < V; ++q) {
+            a.post_w.load(cols, 0, q, through[q]);
+            if (kind == kGateNone || kind == kGateElement) continue;
+            Pair g[4];
+            a.gate.load(cols, gate_row(a, row), q, g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) through[q][i] = through[q][i] * g[i];
+        }
     };
-    auto load = [&](int64_t row, BackRow<S, B> &in) {
-        cols.load(static_cast<const B *>(a.dh) + row * a.ld_dh, 0, in.dh);
-        cols.load(static_cast<const S *>(a.y) + row * a.ld_y, 0, in.y);
-        if (a.dy) cols.load(static_cast<const S *>(a.dy) + row * a.ld_dy, 0, in.dy); else in.dy.zero();
-        cols.load(static_cast<const B *>(a.f) + row * a.ld_f, 0, in.f);
-        in.sf = __ldg(a.stats + row);
-        in.sy = __ldg(a.stats + a.rows + row);
+    // where a thread's pieces of tensor n (dh, y, dy, f) lie
+    constexpr int kB = sizeof(B) / 2, kS = sizeof(S) / 2;
+    auto piece = [&](int buffer, int q, int n) {
+        const int p = n == 0 ? 0 : n == 1 ? kB : n == 2 ? kB + kS : kB + 2 * kS;
+        return incoming + (((buffer * V + q) * kPieces + p) * kBlock + threadIdx.x) * 16;
+    };
+    auto copy = [&](auto *row, int64_t ld, int64_t r, int buffer, int n) {
+        using T = typename std::remove_const<typename std::remove_pointer<decltype(row)>::type>::type;
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+            if (cols.valid(q, 0)) {
+#pragma unroll
+                for (int k = 0; k < static_cast<int>(sizeof(T) / 2); ++k)
+                    copy_async16(piece(buffer, q, n) + k * kBlock * 16,
+                                 reinterpret_cast<const char *>(row + r * ld + cols.at(q, 0)) + 16 * k);
+            }
+    };
+    auto fetch = [&](int64_t n) {
+        const int64_t r = first + n * step;
+        if (VEC && r < end) {
+            copy(static_cast<const B *>(a.dh), a.ld_dh, r, n % kAhead, 0);
+            copy(static_cast<const S *>(a.y), a.ld_y, r, n % kAhead, 1);
+            if (a.dy) copy(static_cast<const S *>(a.dy), a.ld_dy, r, n % kAhead, 2);
+            copy(static_cast<const B *>(a.f), a.ld_f, r, n % kAhead, 3);
+        }
+        copies_commit();
+    };
+    // a group of columns of tensor n of row r, from shared memory or (not VEC) from memory
+    auto take = [&](auto &e, auto *row, int64_t ld, int64_t r, bool live, int buffer, int q, int n) {
+        if (!live || (VEC && !cols.valid(q, 0))) {
+            e.zero();
+        } else if constexpr (VEC) {
+            e.from_shared(piece(buffer, q, n), kBlock * 16);
+        } else {
+            cols.load(row + r * ld, q, e);
+        }
     };
     // row k of the workspace's array n (0: A, 1: B, then S and D)
     auto place = [&](int n, int64_t k) {
@@ -128,142 +170,188 @@ __global__ void __launch_bounds__(32 * W * G, W == 16 ? 1 : 2) peri_backward_ker
     };
     // what S and D hold at the end of gate row g
     auto end_gate = [&](int64_t g) {
-        float gate[8], w[8], b[8], out[8];
-        if (a.split) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (cols.valid(0, i)) {
-                    place(2, worker + g)[cols.at(0, i)] = sum[1][i];
-                    if (FULL) place(3, worker + g)[cols.at(0, i)] = sum[FULL ? 3 : 0][i];
+        for (int q = 0; q < V; ++q) {
+            float gate[8], w[8], b[8], out[8];
+            if (a.split) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (cols.valid(q, i)) {
+                        place(2, worker + g)[cols.at(q, i)] = at(sum[1][q], i);
+                        if (FULL) place(3, worker + g)[cols.at(q, i)] = at(sum[FULL ? 3 : 0][q], i);
+                    }
+            } else {
+                a.gate.load(cols, g * a.d, q, gate);
+                a.post_w.load(cols, 0, q, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[i] = w[i] * at(sum[1][q], i);
+                if (FULL && a.post_b.p) {
+                    a.post_b.load(cols, 0, q, b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) out[i] = fmaf(b[i], at(sum[FULL ? 3 : 0][q], i), out[i]);
                 }
-        } else {
-            a.gate.load(cols, g * a.d, 0, gate);
-            a.post_w.load(cols, 0, 0, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = w[i] * sum[1][i], b[i] = 0.0f;
-            if (FULL && a.post_b.p) {
-                a.post_b.load(cols, 0, 0, b);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) out[i] = fmaf(b[i], sum[FULL ? 3 : 0][i], out[i]);
+                for (int i = 0; i < 8; ++i)
+                    if (cols.valid(q, i)) {
+                        a.d_gate.set(g * a.d + cols.at(q, i), out[i]);
+                        // the weight's and the bias's sums go on in the worker's place
+                        place(2, worker)[cols.at(q, i)] += gate[i] * at(sum[1][q], i);
+                        if (FULL) place(3, worker)[cols.at(q, i)] += gate[i] * at(sum[FULL ? 3 : 0][q], i);
+                    }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (cols.valid(0, i)) {
-                    a.d_gate.set(g * a.d + cols.at(0, i), out[i]);
-                    // the weight's and the bias's sums go on in the worker's place
-                    place(2, worker)[cols.at(0, i)] += gate[i] * sum[1][i];
-                    if (FULL) place(3, worker)[cols.at(0, i)] += gate[i] * sum[FULL ? 3 : 0][i];
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sum[1][i] = 0.0f;
-            if (FULL) sum[FULL ? 3 : 0][i] = 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                sum[1][q][i] = Pair(0.0f);
+                if (FULL) sum[FULL ? 3 : 0][q][i] = Pair(0.0f);
+            }
         }
     };
 
     if constexpr (C > 1) cooperative_groups::this_cluster().sync();   // every block of the cluster runs
-    set_gate(min(r, a.rows - 1));
-    int64_t g = kind == kGateRows ? r / a.per_gate : 0, g_end = (g + 1) * a.per_gate;
-    BackRow<S, B> now, next;
-    if (r < end) load(r, now);
-    for (; r < end; r += step) {
-        if (r + step < end) load(r + step, next);
-        float each[8], w[8], b[8];
-        if (kind == kGateElement) a.gate.load(cols, r * a.d, 0, each);
-        float q[8], t[8], v1[FULL ? 2 : 1] = {};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float dh = now.dh.get(i), n = (now.y.get(i) - now.sy.x) * now.sy.y;
-            q[i] = dh * pre_w[i];
-            t[i] = n;
-            v1[0] = fmaf(q[i], n, v1[0]);
-            sum[0][i] = fmaf(dh, n, sum[0][i]);
-            if (FULL) {
-                v1[FULL ? 1 : 0] += q[i];
-                sum[FULL ? 2 : 0][i] += dh;
+    for (int n = 0; n < kAhead - 1; ++n) fetch(n);
+    set_gate(min(first, a.rows - 1));
+    int64_t g = kind == kGateRows ? first / a.per_gate : 0, g_end = (g + 1) * a.per_gate;
+    for (int64_t n = 0; n < rounds; ++n) {
+        const int64_t r = first + n * step;
+        const bool live = r < end;
+        const int buffer = n % kAhead;
+        float2 sf = make_float2(0.0f, 0.0f), sy = make_float2(0.0f, 0.0f);
+        if (live) sy = __ldg(a.stats + a.rows + r), sf = __ldg(a.stats + r);
+        fetch(n + kAhead - 1);
+        copies_wait<kAhead - 1>();
+        Pair u[V][4], t[V][4], two[FULL ? 2 : 1];
+        two[0] = two[FULL ? 1 : 0] = Pair(0.0f);
+        // a normalised value: (z - mean) r (z r - mean r would lose what z and a large mean have in common)
+        const Pair ry(sy.y), sub_y(-sy.x), rf(sf.y), sub_f(-sf.x);
+        auto normal = [](Pair z, Pair r, Pair sub) { return FULL ? (z + sub) * r : z * r; };
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            Eight<B> dh;
+            Eight<S> y;
+            take(dh, static_cast<const B *>(a.dh), a.ld_dh, r, live, buffer, q, 0);
+            take(y, static_cast<const S *>(a.y), a.ld_y, r, live, buffer, q, 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Pair h = dh.pair(i), m = normal(y.pair(i), ry, sub_y);
+                u[q][i] = h * pre_w[q][i];
+                t[q][i] = m;
+                two[0] = fma2(u[q][i], m, two[0]);
+                sum[0][q][i] = fma2(h, m, sum[0][q][i]);
+                if (FULL) {
+                    two[FULL ? 1 : 0] = two[FULL ? 1 : 0] + u[q][i];
+                    sum[FULL ? 2 : 0][q][i] = sum[FULL ? 2 : 0][q][i] + h;
+                }
             }
         }
-        sums.add(v1, 0);
-        const float m1 = v1[0] * inv_d, m2 = FULL && a.layer ? v1[FULL ? 1 : 0] * inv_d : 0.0f;
-        float out[8], v2[FULL ? 2 : 1] = {};
+        float v[FULL ? 2 : 1];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            t[i] = fmaf(now.sy.y, q[i] - t[i] * m1 - m2, now.dy.get(i));              // dY
-            out[i] = a.residual_scale * t[i];
-        }
-        cols.store(static_cast<S *>(a.dx) + r * a.ld_dx, 0, out);
-        if (kind == kGateElement) {
-            a.post_w.load(cols, 0, 0, w);
-            if (FULL && a.post_b.p) a.post_b.load(cols, 0, 0, b);
+        for (int i = 0; i < (FULL ? 2 : 1); ++i) v[i] = two[i].lo() + two[i].hi();
+        sums.add(v, 0);
+        // dY = dy + r (u - n mean(u n) [- mean(u)])
+        const Pair by_n(-sy.y * (v[0] * inv_d)), by_1(FULL && a.layer ? -sy.y * (v[FULL ? 1 : 0] * inv_d) : 0.0f);
+        two[0] = two[FULL ? 1 : 0] = Pair(0.0f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float z = (now.f.get(i) - now.sf.x) * now.sf.y * w[i];
-                if (FULL && a.post_b.p) z += b[i];
-                out[i] = t[i] * z;
-                t[i] *= each[i];                                                     // dz
+        for (int q = 0; q < V; ++q) {
+            Eight<S> dy;
+            Eight<B> f;
+            Pair out[4], each[4], w[4], b[4];
+            if (a.dy) take(dy, static_cast<const S *>(a.dy), a.ld_dy, r, live, buffer, q, 2); else dy.zero();
+            take(f, static_cast<const B *>(a.f), a.ld_f, r, live, buffer, q, 3);
+            if (kind == kGateElement && live) a.gate.load(cols, r * a.d, q, each);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                Pair s = fma2(t[q][i], by_n, dy.pair(i));
+                if (FULL) s = s + by_1;
+                t[q][i] = fma2(u[q][i], ry, s);
+                out[i] = t[q][i] * Pair(a.residual_scale);
             }
-            if (VEC) {
-                if (a.d_gate.bf16) cols.store(static_cast<Bf16 *>(a.d_gate.p) + r * a.d, 0, out);
-                else cols.store(static_cast<float *>(a.d_gate.p) + r * a.d, 0, out);
-            } else {
+            if (live) cols.store(static_cast<S *>(a.dx) + r * a.ld_dx, q, out);
+            if (kind == kGateElement && live) {
+                a.post_w.load(cols, 0, q, w);
+                if (FULL && a.post_b.p) a.post_b.load(cols, 0, q, b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (cols.valid(0, i)) a.d_gate.set(r * a.d + cols.at(0, i), out[i]);
+                for (int i = 0; i < 4; ++i) {
+                    Pair z = normal(f.pair(i), rf, sub_f) * w[i];
+                    if (FULL && a.post_b.p) z = z + b[i];
+                    out[i] = t[q][i] * z;
+                    t[q][i] = t[q][i] * each[i];                                         // dz
+                }
+                if (VEC) {
+                    if (a.d_gate.bf16) cols.store(static_cast<Bf16 *>(a.d_gate.p) + r * a.d, q, out);
+                    else cols.store(static_cast<float *>(a.d_gate.p) + r * a.d, q, out);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (cols.valid(q, i)) a.d_gate.set(r * a.d + cols.at(q, i), at(out, i));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Pair m = normal(f.pair(i), rf, sub_f);
+                sum[1][q][i] = fma2(t[q][i], m, sum[1][q][i]);
+                if (FULL) sum[FULL ? 3 : 0][q][i] = sum[FULL ? 3 : 0][q][i] + t[q][i];
+                u[q][i] = t[q][i] * through[q][i];
+                t[q][i] = m;
+                two[0] = fma2(u[q][i], m, two[0]);
+                if (FULL) two[FULL ? 1 : 0] = two[FULL ? 1 : 0] + u[q][i];
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float n = (now.f.get(i) - now.sf.x) * now.sf.y;
-            sum[1][i] = fmaf(t[i], n, sum[1][i]);
-            if (FULL) sum[FULL ? 3 : 0][i] += t[i];
-            q[i] = t[i] * through[i];
-            v2[0] = fmaf(q[i], n, v2[0]);
-            if (FULL) v2[FULL ? 1 : 0] += q[i];
-        }
-        sums.add(v2, 1);
-        const float m3 = v2[0] * inv_d, m4 = FULL && a.layer ? v2[FULL ? 1 : 0] * inv_d : 0.0f;
+        for (int i = 0; i < (FULL ? 2 : 1); ++i) v[i] = two[i].lo() + two[i].hi();
+        sums.add(v, 1);
+        const Pair df_n(-sf.y * (v[0] * inv_d)), df_1(FULL && a.layer ? -sf.y * (v[FULL ? 1 : 0] * inv_d) : 0.0f);
+        if (live) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float n = (now.f.get(i) - now.sf.x) * now.sf.y;
-            out[i] = now.sf.y * (q[i] - n * m3 - m4);
-        }
-        cols.store(static_cast<B *>(a.df) + r * a.ld_df, 0, out);
-        if (kind == kGateRows) {
-            const bool last = r + 1 == end;
-            if (last || r + 1 == g_end) {
-                end_gate(g);
-                ++g, g_end += a.per_gate;
-                if (!last) set_gate(r + 1);
+            for (int q = 0; q < V; ++q) {
+                Pair out[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    out[i] = FULL ? fma2(t[q][i], df_n, df_1) : t[q][i] * df_n;
+                    out[i] = fma2(u[q][i], rf, out[i]);
+                }
+                cols.store(static_cast<B *>(a.df) + r * a.ld_df, q, out);
+            }
+            if (kind == kGateRows) {
+                const bool last = r + 1 == end;
+                if (last || r + 1 == g_end) {
+                    end_gate(g);
+                    ++g, g_end += a.per_gate;
+                    if (!last) set_gate(r + 1);
+                }
             }
         }
-        now = next;
     }
+    copies_wait<0>();
 
     // the block's rows of the workspace: its groups' sums, added in their order
     __syncthreads();
+    float *joined = reinterpret_cast<float *>(incoming);
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         if (k % 2 == 1 && kind == kGateRows) continue;             // S and D are there already
         const int array = kSums == 2 ? 2 * k : k % 2 * 2 + k / 2;    // A 0, B 1, S 2, D 3
-        if constexpr (G > 1) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) joined[threadIdx.x * 8 + i] = sum[k][i];
-            __syncthreads();
-            if (group == 0) {
+        for (int q = 0; q < V; ++q) {
+            if constexpr (G > 1) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float v = 0.0f;
+                for (int i = 0; i < 8; ++i) joined[i * kBlock + threadIdx.x] = at(sum[k][q], i);
+                __syncthreads();
+                if (group == 0) {
 #pragma unroll
-                    for (int g = 0; g < G; ++g) v += joined[(g * 32 * W + threadIdx.x) * 8 + i];
-                    if (cols.valid(0, i)) place(array, block)[cols.at(0, i)] = v;
+                    for (int i = 0; i < 8; ++i) {
+                        float v = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < G; ++j) v += joined[i * kBlock + j * kThreads + threadIdx.x];
+                        if (cols.valid(q, i)) place(array, block)[cols.at(q, i)] = v;
+                    }
                 }
-            }
-            __syncthreads();
-        } else {
+                __syncthreads();
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (cols.valid(0, i)) place(array, block)[cols.at(0, i)] = sum[k][i];
+                for (int i = 0; i < 8; ++i)
+                    if (cols.valid(q, i)) place(array, block)[cols.at(q, i)] = at(sum[k][q], i);
+            }
         }
     }
     if constexpr (C > 1) cooperative_groups::this_cluster().sync();   // nobody's shared memory goes while it may be written
@@ -332,13 +420,24 @@ __global__ void __launch_bounds__(256) peri_backward_sums_kernel(const NormArgs 
     }
 }
 
-template <typename S, typename B, int W, int C, bool VEC>
+// Which of the two kernels a shape is run by: without or with the means and the sums of dh and dY.
+enum { kPlain, kFull, kEither };
+
+template <typename S, typename B, int V, int W, int L, int C, bool VEC, int KIND>
 cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaStream_t stream) {
-    constexpr int G = W == 1 ? 8 : W == 2 ? 4 : W <= 4 ? 2 : 1;
-    auto kernel = a.layer || a.post_b.p ? peri_backward_kernel<S, B, W, G, C, VEC, true> : peri_backward_kernel<S, B, W, G, C, VEC, false>;
+    constexpr int kBlock = kBackThreads<W>;
+    constexpr int kJoin = kBlock * 8 * 4, kLand = VEC ? 2 * V * static_cast<int>(sizeof(S) + sizeof(B)) * kBlock * 16 : 0;
+    constexpr int kBytes = kLand > kJoin ? kLand : kJoin;
+    auto kernel = KIND == kFull || (KIND == kEither && p.full) ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain>
+                                                               : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull>;
+    if (kBytes > 40 * 1024) {                          // with the static part, over what needs no asking
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(static_cast<unsigned>(p.blocks * C));
-    config.blockDim = dim3(32 * W * G);
+    config.blockDim = dim3(kBlock);
+    config.dynamicSmemBytes = kBytes;
     config.stream = stream;
     cudaLaunchAttribute cluster;
     cluster.id = cudaLaunchAttributeClusterDimension;
@@ -356,7 +455,6 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
     NormArgs a = args;
     const BackwardPlan p = plan_backward(a, vec);
     a.contiguous = p.contiguous, a.split = p.split;
-    const bool full = a.layer || a.post_b.p;
     const int64_t workers = p.blocks * p.groups;
     cudaError_t e = cudaSuccess;
     if (a.rows == 0 || (p.contiguous && !p.split)) {   // nothing writes the sums, or they grow in place
@@ -364,27 +462,37 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
         if (e != cudaSuccess) return e;
     }
     if (a.rows > 0) {
-        if (p.cluster > 1) {
-            e = vec ? (p.cluster == 2 ? launch_backward_rows<S, B, 16, 2, true>(a, p, stream)
-                                      : launch_backward_rows<S, B, 16, 4, true>(a, p, stream))
-                    : launch_backward_rows<S, B, 16, 4, false>(a, p, stream);
-        } else if (!vec) {
-            e = p.warps == 1   ? launch_backward_rows<S, B, 1, 1, false>(a, p, stream)
-                : p.warps == 4 ? launch_backward_rows<S, B, 4, 1, false>(a, p, stream)
-                               : launch_backward_rows<S, B, 16, 1, false>(a, p, stream);
-        } else {
-            switch (p.warps) {
-                case 1: e = launch_backward_rows<S, B, 1, 1, true>(a, p, stream); break;
-                case 2: e = launch_backward_rows<S, B, 2, 1, true>(a, p, stream); break;
-                case 3: e = launch_backward_rows<S, B, 3, 1, true>(a, p, stream); break;
-                case 4: e = launch_backward_rows<S, B, 4, 1, true>(a, p, stream); break;
-                case 8: e = launch_backward_rows<S, B, 8, 1, true>(a, p, stream); break;
-                default: e = launch_backward_rows<S, B, 16, 1, true>(a, p, stream); break;
-            }
+        switch ((vec ? 0 : 100000) + p.groups_of_eight * 10000 + p.cluster * 1000 + (p.warps == 1 ? p.lanes : 32 * p.warps)) {
+#define MTDAO_BACKWARD_CASE(V, W, L, C, VEC, FULL)                                  \
+    case (VEC ? 0 : 100000) + V * 10000 + C * 1000 + (W == 1 ? L : 32 * W):         \
+        e = launch_backward_rows<S, B, V, W, L, C, VEC, FULL>(a, p, stream);        \
+        break;
+            MTDAO_BACKWARD_CASE(1, 1, 8, 1, true, kEither)
+            MTDAO_BACKWARD_CASE(1, 1, 16, 1, true, kEither)
+            MTDAO_BACKWARD_CASE(1, 1, 32, 1, true, kEither)
+            MTDAO_BACKWARD_CASE(2, 1, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 2, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 4, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 8, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 8, 32, 2, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 8, 32, 4, true, kPlain)
+            MTDAO_BACKWARD_CASE(1, 2, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 3, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 4, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 8, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 16, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 16, 32, 2, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 16, 32, 4, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 1, 32, 1, false, kFull)
+            MTDAO_BACKWARD_CASE(1, 4, 32, 1, false, kFull)
+            MTDAO_BACKWARD_CASE(1, 16, 32, 1, false, kFull)
+            MTDAO_BACKWARD_CASE(1, 16, 32, 4, false, kFull)
+#undef MTDAO_BACKWARD_CASE
+            default: return cudaErrorInvalidValue;
         }
         if (e != cudaSuccess) return e;
     }
-    peri_backward_sums_kernel<S><<<(a.d + 31) / 32, 256, 0, stream>>>(a, p.blocks, workers, full);
+    peri_backward_sums_kernel<S><<<(a.d + 31) / 32, 256, 0, stream>>>(a, p.blocks, workers, a.layer || a.post_b.p);
     return cudaGetLastError();
 }
 
