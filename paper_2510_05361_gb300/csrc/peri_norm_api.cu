@@ -13,7 +13,7 @@
 
 namespace mtdao {
 
-// A thread has sixteen columns of a row where it keeps two sums for each, else eight (four sums of sixteen are more than
+// A thread has sixteen columns of a long row where it keeps two sums for each, else eight (four sums of sixteen are more than
 // its registers hold); rows too long for one thread block are spread over a cluster of them.  512 threads an
 // SM; fewer where rows run out.
 BackwardPlan plan_backward(const NormArgs &a, bool vec) {
@@ -26,7 +26,7 @@ BackwardPlan plan_backward(const NormArgs &a, bool vec) {
         p.cluster = a.d <= 4096 ? 1 : 4;
     } else if (a.d <= 256) {
         p.lanes = a.d <= 64 ? 8 : a.d <= 128 ? 16 : 32;
-    } else if (p.full) {
+    } else if (p.full || a.d <= 1024) {
         const int need = (a.d + 255) / 256;
         p.warps = need <= 4 ? need : need <= 8 ? 8 : 16;
         while (4096 * p.cluster < a.d) p.cluster *= 2;

@@ -78,6 +78,11 @@ struct RowSums {
 template <int W>
 constexpr int kBackThreads = W == 3 ? 96 : W <= 4 ? 128 : 32 * W;
 
+// Rows that are in shared memory or on their way: with eight columns a thread a row for each worker is
+// too little to keep the memory busy (32 KB an SM in bf16).
+template <int V>
+constexpr int kRowsAhead = V == 1 ? 3 : 2;
+
 // V groups of eight columns a thread.  FULL: "layer" norm or biases; else the sums of dh and dY and the means are
 // left out.
 template <typename S, typename B, int V, int W, int L, int C, bool VEC, bool FULL>
@@ -85,7 +90,7 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
     constexpr int kSums = FULL ? 4 : 2;                 // A, S or A, S, B, D
     constexpr int kBlock = kBackThreads<W>, kThreads = W == 1 ? L : 32 * W, G = kBlock / kThreads;
     constexpr int kPieces = 2 * (static_cast<int>(sizeof(S)) + static_cast<int>(sizeof(B))) / 2;     // of 16 bytes, of a group of columns
-    constexpr int kAhead = 2;
+    constexpr int kAhead = kRowsAhead<V>;
     extern __shared__ __align__(16) char incoming[];    // [kAhead][V][kPieces][threads][16]
     __shared__ RowSums<W, L, G, C> sums;
     const int group = threadIdx.x / kThreads;
@@ -208,6 +213,13 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
     };
 
     if constexpr (C > 1) cooperative_groups::this_cluster().sync();   // every block of the cluster runs
+    float2 next_sf, next_sy;
+    auto ask_stats = [&](int64_t n) {
+        const int64_t r = first + n * step;
+        next_sf = next_sy = make_float2(0.0f, 0.0f);
+        if (r < end) next_sy = __ldg(a.stats + a.rows + r), next_sf = __ldg(a.stats + r);
+    };
+    ask_stats(0);
 #pragma unroll
     for (int n = 0; n < kAhead - 1; ++n) fetch(n);
     set_gate(min(first, a.rows - 1));
@@ -216,8 +228,8 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
         const int64_t r = first + n * step;
         const bool live = r < end;
         const int buffer = n % kAhead;
-        float2 sf = make_float2(0.0f, 0.0f), sy = make_float2(0.0f, 0.0f);
-        if (live) sy = __ldg(a.stats + a.rows + r), sf = __ldg(a.stats + r);
+        const float2 sf = next_sf, sy = next_sy;
+        ask_stats(n + 1);
         fetch(n + kAhead - 1);
         copies_wait<kAhead - 1>();
         Pair u[V][4], t[V][4], two[FULL ? 2 : 1];
@@ -357,66 +369,69 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
     if constexpr (C > 1) cooperative_groups::this_cluster().sync();   // nobody's shared memory goes while it may be written
 }
 
-// The sums over the workspace's rows, 32 columns a thread block, eight threads a column.
+// The sums over the workspace's rows: 32 columns a thread block, 32 threads a column.
 template <typename S>
-__global__ void __launch_bounds__(256) peri_backward_sums_kernel(const NormArgs a, int64_t blocks, int64_t workers, bool full) {
-    __shared__ float parts[8][33];
+__global__ void __launch_bounds__(1024) peri_backward_sums_kernel(const NormArgs a, int64_t blocks, int64_t workers, bool full) {
+    constexpr int kParts = 32;
+    __shared__ float parts[4][kParts][33];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
     const bool valid = c < a.d;
     const int kind = gate_kind(a);
-    auto reduce = [&](float v) {
-        __syncthreads();
-        parts[part][threadIdx.x & 31] = v;
-        __syncthreads();
-        float t = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t += parts[i][threadIdx.x & 31];
-        return t;
-    };
-    auto column = [&](const float *p, int64_t lo, int64_t hi) {
-        float v = 0.0f;
-        if (valid)
-            for (int64_t k = lo + part; k < hi; k += 8) v += p[k * a.d + c];
-        return reduce(v);
-    };
-    const float *A = a.partial, *Bs = A + blocks * a.d, *Ss = Bs + blocks * a.d;
-    const int64_t rows = kind == kGateRows ? (a.split ? workers + a.gate_rows : workers) : blocks;
+    const bool split = kind == kGateRows && a.split;
+    const float *A = a.partial + (valid ? c : 0), *B = A + blocks * a.d, *Ss = B + blocks * a.d;
+    const int64_t rows = kind != kGateRows ? blocks : split ? workers + a.gate_rows : workers;
     const float *Ds = Ss + rows * a.d;
-    const float pre_w = column(A, 0, blocks), pre_b = full ? column(Bs, 0, blocks) : 0.0f;
-    float post_w = 0.0f, post_b = 0.0f;
-    if (kind == kGateRows && a.split) {
-        const float w = valid ? a.post_w.get(c) : 0.0f, b = valid && a.post_b.p ? a.post_b.get(c) : 0.0f;
+    float v[4] = {};                                   // of dh n_y, dh, dz n_f, dz
+    auto add = [&](const float *p, const float *q, int64_t count, float &x, float &y) {
+#pragma unroll 8
+        for (int64_t k = part; k < count; k += kParts) {
+            x += p[k * a.d];
+            if (full) y += q[k * a.d];
+        }
+    };
+    add(A, B, blocks, v[0], v[1]);
+    if (!split) {
+        add(Ss, Ds, rows, v[2], v[3]);
+    } else if (valid) {
+        const float w = a.post_w.get(c), b = a.post_b.p ? a.post_b.get(c) : 0.0f;
         const int64_t most = (a.rows + workers - 1) / workers;         // rows of a worker
-        for (int64_t g = part; valid && g < a.gate_rows; g += 8) {      // gate rows over the column's threads
+        for (int64_t g = part; g < a.gate_rows; g += kParts) {          // gate rows over the column's threads
             const int64_t lo = g * a.per_gate / most + g, hi = ((g + 1) * a.per_gate - 1) / most + g + 1;
             float s = 0.0f, d = 0.0f;
+#pragma unroll 4
             for (int64_t k = lo; k < hi; ++k) {
-                s += Ss[k * a.d + c];
-                if (full) d += Ds[k * a.d + c];
+                s += Ss[k * a.d];
+                if (full) d += Ds[k * a.d];
             }
             const float gate = a.gate.get(g * a.d + c);
-            post_w = fmaf(gate, s, post_w);
-            post_b = fmaf(gate, d, post_b);
+            v[2] = fmaf(gate, s, v[2]);
+            v[3] = fmaf(gate, d, v[3]);
             a.d_gate.set(g * a.d + c, fmaf(w, s, b * d));
         }
-        post_w = reduce(post_w);
-        post_b = reduce(post_b);
-    } else {
-        post_w = column(Ss, 0, rows);
-        post_b = full ? column(Ds, 0, rows) : 0.0f;
-        if (kind == kGateChannel && valid) {
-            const float gate = a.gate.get(c), b = a.post_b.p ? a.post_b.get(c) : 0.0f;
-            if (part == 0) a.d_gate.set(c, fmaf(a.post_w.get(c), post_w, b * post_b));
-            post_w *= gate;
-            post_b *= gate;
-        }
     }
-    if (!valid || part != 0) return;
-    a.d_pre_w.set(c, pre_w);
-    a.d_post_w.set(c, post_w);
-    if (a.post_b.p) {
-        a.d_pre_b.set(c, pre_b);
-        a.d_post_b.set(c, post_b);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) parts[k][part][threadIdx.x & 31] = v[k];
+    __syncthreads();
+    if (part >= 4) return;
+    // a warp for each of the four, a lane for each column
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) t += parts[part][i][threadIdx.x & 31];
+    if (!valid) return;
+    if (part == 0) a.d_pre_w.set(c, t);
+    if (part == 1 && a.post_b.p) a.d_pre_b.set(c, t);
+    const float gate = kind == kGateChannel && part >= 2 ? a.gate.get(c) : 1.0f;
+    if (part == 2) a.d_post_w.set(c, t * gate);
+    if (part == 3 && a.post_b.p) a.d_post_b.set(c, t * gate);
+    if (kind == kGateChannel && part == 2) {
+        float s = t * a.post_w.get(c);
+        if (a.post_b.p) {
+            float d = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) d += parts[3][i][threadIdx.x & 31];
+            s = fmaf(a.post_b.get(c), d, s);
+        }
+        a.d_gate.set(c, s);
     }
 }
 
@@ -426,7 +441,7 @@ enum { kPlain, kFull, kEither };
 template <typename S, typename B, int V, int W, int L, int C, bool VEC, int KIND>
 cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaStream_t stream) {
     constexpr int kBlock = kBackThreads<W>;
-    constexpr int kJoin = kBlock * 8 * 4, kLand = VEC ? 2 * V * static_cast<int>(sizeof(S) + sizeof(B)) * kBlock * 16 : 0;
+    constexpr int kJoin = kBlock * 8 * 4, kLand = VEC ? kRowsAhead<V> * V * static_cast<int>(sizeof(S) + sizeof(B)) * kBlock * 16 : 0;
     constexpr int kBytes = kLand > kJoin ? kLand : kJoin;
     auto kernel = KIND == kFull || (KIND == kEither && p.full) ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain>
                                                                : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull>;
@@ -470,15 +485,13 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
             MTDAO_BACKWARD_CASE(1, 1, 8, 1, true, kEither)
             MTDAO_BACKWARD_CASE(1, 1, 16, 1, true, kEither)
             MTDAO_BACKWARD_CASE(1, 1, 32, 1, true, kEither)
-            MTDAO_BACKWARD_CASE(2, 1, 32, 1, true, kPlain)
-            MTDAO_BACKWARD_CASE(2, 2, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 4, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 2, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 4, true, kPlain)
-            MTDAO_BACKWARD_CASE(1, 2, 32, 1, true, kFull)
-            MTDAO_BACKWARD_CASE(1, 3, 32, 1, true, kFull)
-            MTDAO_BACKWARD_CASE(1, 4, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 2, 32, 1, true, kEither)
+            MTDAO_BACKWARD_CASE(1, 3, 32, 1, true, kEither)
+            MTDAO_BACKWARD_CASE(1, 4, 32, 1, true, kEither)
             MTDAO_BACKWARD_CASE(1, 8, 32, 1, true, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 1, true, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 2, true, kFull)
@@ -492,7 +505,7 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
         }
         if (e != cudaSuccess) return e;
     }
-    peri_backward_sums_kernel<S><<<(a.d + 31) / 32, 256, 0, stream>>>(a, p.blocks, workers, a.layer || a.post_b.p);
+    peri_backward_sums_kernel<S><<<(a.d + 31) / 32, 1024, 0, stream>>>(a, p.blocks, workers, a.layer || a.post_b.p);
     return cudaGetLastError();
 }
 
