@@ -58,7 +58,7 @@ struct Eight<Bf16> {
         for (int i = 0; i < 4; ++i) w[i] = bf16x2(x[2 * i], x[2 * i + 1]);
     }
     __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
-    __device__ __forceinline__ void from_shared(const char *at, int apart) {      // pieces of 16 bytes
+    __device__ __forceinline__ void from_shared(const char *at) {
         const uint4 q = *reinterpret_cast<const uint4 *>(at);
         w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
     }
@@ -91,8 +91,8 @@ struct Eight<float> {
         for (int i = 0; i < 8; ++i) w[i] = 0.0f;
     }
     __device__ __forceinline__ void put(int i, float x) { w[i] = x; }
-    __device__ __forceinline__ void from_shared(const char *at, int apart) {
-        const float4 a = *reinterpret_cast<const float4 *>(at), b = *reinterpret_cast<const float4 *>(at + apart);
+    __device__ __forceinline__ void from_shared(const char *at) {
+        const float4 a = *reinterpret_cast<const float4 *>(at), b = *reinterpret_cast<const float4 *>(at + 16);
         w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
     }
     __device__ __forceinline__ void load(const float *p) {

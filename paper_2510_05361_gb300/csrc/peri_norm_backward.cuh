@@ -4,7 +4,7 @@
 // worker: the lanes or warps of one row, in one thread block or a cluster of them), so that the sums over rows which
 // the weights' gradients are stay in its registers; a row's own two sums (of the norm before the
 // block, then of the one after it) go over the worker's warps.  The next row is on its way to
-// shared memory while one is worked on; a thread reads only what it copied itself.
+// shared memory while one is worked on; a warp reads only what it copied itself.
 // Four sums a column: of dh n_y, dh, dY n_f, dY, from which a gate that is the
 // same for the rows summed gives its own gradient and the norm's (post_w S is the gate's, gate S the weight's).
 //
@@ -131,22 +131,29 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
             for (int i = 0; i < 4; ++i) through[q][i] = through[q][i] * g[i];
         }
     };
-    // where a thread's pieces of tensor n (dh, y, dy, f) lie
-    constexpr int kB = sizeof(B) / 2, kS = sizeof(S) / 2;
-    auto piece = [&](int buffer, int q, int n) {
+    // Where tensor n (dh, y, dy, f) of a group of columns lies: its threads' columns side by side.  A
+    // row's lanes copy them in pieces of 16 bytes that follow one another (in fp32 not each lane its own
+    // 32 bytes: every 32-byte sector would be fetched twice).
+    constexpr int kB = sizeof(B) / 2, kS = sizeof(S) / 2, kLanes = W == 1 ? L : 32;
+    const int lane = static_cast<int>(threadIdx.x) % kLanes;
+    auto region = [&](int buffer, int q, int n) {
         const int p = n == 0 ? 0 : n == 1 ? kB : n == 2 ? kB + kS : kB + 2 * kS;
-        return incoming + (((buffer * V + q) * kPieces + p) * kBlock + threadIdx.x) * 16;
+        return incoming + ((buffer * V + q) * kPieces + p) * kBlock * 16;
     };
     auto copy = [&](auto *row, int64_t ld, int64_t r, int buffer, int n) {
         using T = typename std::remove_const<typename std::remove_pointer<decltype(row)>::type>::type;
+        constexpr int kEach = sizeof(T) / 2, kColumns = 8 / kEach;
 #pragma unroll
-        for (int q = 0; q < V; ++q)
-            if (cols.valid(q, 0)) {
+        for (int q = 0; q < V; ++q) {
+            const int start = (q * cols.threads + cols.t - lane) * 8;
 #pragma unroll
-                for (int k = 0; k < static_cast<int>(sizeof(T) / 2); ++k)
-                    copy_async16(piece(buffer, q, n) + k * kBlock * 16,
-                                 reinterpret_cast<const char *>(row + r * ld + cols.at(q, 0)) + 16 * k);
+            for (int k = 0; k < kEach; ++k) {
+                const int piece = k * kLanes + lane, c = start + piece * kColumns;
+                if (c < a.d)
+                    copy_async16(region(buffer, q, n) + ((threadIdx.x - lane) * kEach + piece) * 16,
+                                 reinterpret_cast<const char *>(row + r * ld + c));
             }
+        }
     };
     auto fetch = [&](int64_t n) {
         const int64_t r = first + n * step;
@@ -163,7 +170,7 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
         if (!live || (VEC && !cols.valid(q, 0))) {
             e.zero();
         } else if constexpr (VEC) {
-            e.from_shared(piece(buffer, q, n), kBlock * 16);
+            e.from_shared(region(buffer, q, n) + threadIdx.x * static_cast<int>(sizeof(e)));
         } else {
             cols.load(row + r * ld, q, e);
         }
@@ -232,6 +239,7 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
         ask_stats(n + 1);
         fetch(n + kAhead - 1);
         copies_wait<kAhead - 1>();
+        __syncwarp();
         Pair u[V][4], t[V][4], two[FULL ? 2 : 1];
         two[0] = two[FULL ? 1 : 0] = Pair(0.0f);
         // a normalised value: (z - mean) r (z r - mean r would lose what z and a large mean have in common)
