@@ -196,6 +196,7 @@ struct Vector {
 struct NormArgs {
     int64_t rows, gate_rows, per_gate;      // per_gate: rows of one gate row
     int32_t d, layer;
+    int32_t wide;                           // all rows are fp32
     float eps, residual_scale;
     int64_t ld_x, ld_f, ld_y, ld_h, ld_dy, ld_dh, ld_dx, ld_df;
     const void *x, *f, *dy, *dh;

@@ -26,6 +26,10 @@ BackwardPlan plan_backward(const NormArgs &a, bool vec) {
         p.cluster = a.d <= 4096 ? 1 : 4;
     } else if (a.d <= 256) {
         p.lanes = a.d <= 64 ? 8 : a.d <= 128 ? 16 : 32;
+    } else if (a.d > 4096 && !a.wide) {                // 16 warps and shared memory for two rows of 8192
+        p.groups_of_eight = 2;
+        p.warps = 16;
+        while (8192 * p.cluster < a.d) p.cluster *= 2;
     } else if (p.full || a.d <= 1024) {
         const int need = (a.d + 255) / 256;
         p.warps = need <= 4 ? need : need <= 8 ? 8 : 16;
@@ -101,6 +105,7 @@ NormArgs arguments(const mtdao_peri_norm *s) {
     a.per_gate = s->gate_rows > 0 && s->rows > 0 ? s->rows / s->gate_rows : 1;
     a.d = s->d;
     a.layer = s->norm == MTDAO_NORM_LAYER;
+    a.wide = s->branch_dtype == MTDAO_F32;
     a.eps = static_cast<float>(s->eps);
     a.residual_scale = static_cast<float>(s->residual_scale);
     a.ld_x = s->ld_x, a.ld_f = s->ld_f, a.ld_y = s->ld_y, a.ld_h = s->ld_h;

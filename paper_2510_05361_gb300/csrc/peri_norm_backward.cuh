@@ -451,6 +451,8 @@ cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaS
     constexpr int kBlock = kBackThreads<W>;
     constexpr int kJoin = kBlock * 8 * 4, kLand = VEC ? kRowsAhead<V> * V * static_cast<int>(sizeof(S) + sizeof(B)) * kBlock * 16 : 0;
     constexpr int kBytes = kLand > kJoin ? kLand : kJoin;
+    if constexpr (kBytes > 220 * 1024) return cudaErrorInvalidValue;      // the plan takes another shape in fp32
+    else {
     auto kernel = KIND == kFull || (KIND == kEither && p.full) ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain>
                                                                : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull>;
     if (kBytes > 40 * 1024) {                          // with the static part, over what needs no asking
@@ -469,6 +471,7 @@ cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaS
     config.attrs = &cluster;
     config.numAttrs = C > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&config, kernel, a);
+    }
 }
 
 }  // namespace
@@ -495,6 +498,8 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
             MTDAO_BACKWARD_CASE(1, 1, 32, 1, true, kEither)
             MTDAO_BACKWARD_CASE(2, 4, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 16, 32, 1, true, kEither)
+            MTDAO_BACKWARD_CASE(2, 16, 32, 2, true, kEither)
             MTDAO_BACKWARD_CASE(2, 8, 32, 2, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 4, true, kPlain)
             MTDAO_BACKWARD_CASE(1, 2, 32, 1, true, kEither)
