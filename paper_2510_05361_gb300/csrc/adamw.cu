@@ -11,6 +11,7 @@
 #include "adamw.h"
 #include "adamw_codes.cuh"
 #include "kahan.cuh"
+#include "launch.cuh"
 #include "replica_mean.cuh"
 
 namespace mtdao {
@@ -277,6 +278,7 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 // way at once, which registers could not hold.  What a block takes there: each tensor's 256 elements,
 // from the 16-byte boundary before them to the one after, then the codes.
 constexpr int kStageBytes = 4 * kAdamwBlock;             // turn_raw's
+constexpr int kMostShared = 227 * 1024;                  // of a thread block: asked for once, used as the list needs
 
 __host__ __device__ __forceinline__ int tensor_bytes(bool bf16) { return bf16 ? 512 + 16 : 1024 + 16; }
 __host__ __device__ __forceinline__ int slot_bytes(bool g16, bool p16) { return tensor_bytes(g16) + tensor_bytes(p16) + 512; }
@@ -318,11 +320,20 @@ __device__ __forceinline__ void read_elements(const char *at, bool bf16, int ske
     for (int i = 0; i < 8; ++i) w[i] = skew & 2 ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
 }
 
+// A replica's clip factor, from the kernel before this one, which may still run (launch.cuh): asked for after
+// the loads of what no kernel is writing then.
+template <bool CLIP>
+__device__ __forceinline__ float clip_factor(const float *clip) {
+    if constexpr (!CLIP) return 1.0f;
+    cudaGridDependencySynchronize();
+    return __ldcg(clip);
+}
+
 // A warp's blocks first, first + 8, ... below end of a record, as many on their way at a time as fit
 // into its part of shared memory.  BF16: bf16 parameters and gradients, aligned: all four.
 template <bool CLIP, bool BF16>
 __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwScalars &sc, const AdamwChunk &c, uint32_t replica,
-                                              float s, int first, int end, char *mine) {
+                                              const float *clip, int first, int end, char *mine) {
     constexpr int kWarps = kAdamwThreads / 32;
     const int lane = threadIdx.x & 31;
     const bool g16 = BF16 || (c.flags & kAdamwGradBf16), p16 = BF16 || (c.flags & kAdamwParamBf16);
@@ -330,7 +341,7 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
     const int p_skew = BF16 ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.p) & 15);
     const int p_at = tensor_bytes(g16), codes_at = p_at + tensor_bytes(p16), slot = slot_bytes(g16, p16);
     const int fit = BF16 ? kAhead : min(kAhead, a.warp_bytes / slot);
-    float scales = 0.0f;
+    float s = 1.0f, scales = 0.0f;
     if (lane < 2 * kAhead) {
         const int b = first + (lane >> 1) * kWarps;
         if (b < end) scales = __ldcs((lane & 1 ? a.v_scale : a.m_scale) + c.block + b);
@@ -361,6 +372,7 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
     if constexpr (BF16) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fetch(i, mine + i * slot);
+        s = clip_factor<CLIP>(clip);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (first + i * kWarps >= end) break;
@@ -374,6 +386,7 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
     } else {
         for (int round = 0; first + round * kWarps < end; round += fit) {
             for (int i = 0; i < fit; ++i) fetch(round + i, mine + i * slot);
+            if (round == 0) s = clip_factor<CLIP>(clip);
             for (int i = 0; i < fit && first + (round + i) * kWarps < end; ++i) {
                 const int later = fit - 1 - i;
                 if (later >= 3) copies_wait<3>();
@@ -399,7 +412,7 @@ __global__ void __launch_bounds__(kAdamwThreads, BITS == 32 || BF16 ? 4 : 3)
     const uint32_t replica = blockIdx.y;
     const AdamwChunk c = load_chunk(a.chunks + replica * a.n_chunks + blockIdx.x);
     const int first = threadIdx.x >> 5;
-    const float s = CLIP ? clip_scale[replica] : 1.0f;
+    const float *s = clip_scale + replica;
     char *mine = shared + first * (BITS == 8 ? a.warp_bytes : kStageBytes);
     int lo = 0, hi = 0;                                // the record's blocks [lo, hi) are streamed
     if constexpr (BITS == 8) {
@@ -415,7 +428,7 @@ __global__ void __launch_bounds__(kAdamwThreads, BITS == 32 || BF16 ? 4 : 3)
         if (b >= lo && b < hi) continue;
         Raw<BITS> r;
         load_block<BITS>(a, c, b, reinterpret_cast<uint32_t *>(mine), r);
-        update_block<BITS, CLIP, false>(a, sc, c, replica, s, b, reinterpret_cast<uint32_t *>(mine), r);
+        update_block<BITS, CLIP, false>(a, sc, c, replica, clip_factor<CLIP>(s), b, reinterpret_cast<uint32_t *>(mine), r);
     }
 }
 
@@ -532,6 +545,7 @@ __global__ void __launch_bounds__(kAdamwThreads, 4) adamw_norm_kernel(const Adam
     }
     int at;
     bool one = true;
+    cudaTriggerProgrammaticLaunchCompletion();         // the step may take the places that come free
     double in_warp = warp_sums_wide(sum, at, one);
     if (__any_sync(0xffffffffu, wide != 0.0)) in_warp += __shfl_sync(0xffffffffu, warp_sum(wide), 0);
     const double in_block = sum_of_warps(in_warp, parts);
@@ -872,16 +886,18 @@ int32_t adamw_chunk(int num_sms, int bits, int64_t elements) {
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.n_chunks), a.M);
-    if (a.bits == 32) {
-        auto kernel = clip_scale ? adamw_step_kernel<32, true, false> : adamw_step_kernel<32, false, false>;
-        kernel<<<grid, kAdamwThreads, kAdamwThreads / 32 * kStageBytes, stream>>>(a, sc, clip_scale);
-        return cudaGetLastError();
+    int bytes = kAdamwThreads / 32 * kStageBytes;
+    auto kernel = clip_scale ? adamw_step_kernel<32, true, false> : adamw_step_kernel<32, false, false>;
+    if (a.bits == 8) {
+        kernel = a.all_bf16 ? (clip_scale ? adamw_step_kernel<8, true, true> : adamw_step_kernel<8, false, true>)
+                            : (clip_scale ? adamw_step_kernel<8, true, false> : adamw_step_kernel<8, false, false>);
+        bytes = kAdamwThreads / 32 * a.warp_bytes;
+        static std::atomic<uint64_t> done[4];
+        const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kMostShared,
+                                           done[2 * (clip_scale != nullptr) + (a.all_bf16 != 0)]);
+        if (e != cudaSuccess) return e;
     }
-    auto kernel = a.all_bf16 ? (clip_scale ? adamw_step_kernel<8, true, true> : adamw_step_kernel<8, false, true>)
-                             : (clip_scale ? adamw_step_kernel<8, true, false> : adamw_step_kernel<8, false, false>);
-    const int bytes = kAdamwThreads / 32 * a.warp_bytes;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return e;
+    if (clip_scale) return launch_early(kernel, grid, kAdamwThreads, bytes, stream, a, sc, clip_scale);
     kernel<<<grid, kAdamwThreads, bytes, stream>>>(a, sc, clip_scale);
     return cudaGetLastError();
 }
@@ -914,7 +930,8 @@ cudaError_t launch_adamw_average(const AdamwList &a, uint32_t mask, cudaStream_t
     }
     auto kernel = a.params_bf16 ? adamw_average_kernel<8, true> : adamw_average_kernel<8, false>;
     const int warp_bytes = average_warp_bytes(a.params_bf16), bytes = kAdamwThreads / 32 * warp_bytes;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static std::atomic<uint64_t> done[2];
+    const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kMostShared, done[a.params_bf16 != 0]);
     if (e != cudaSuccess) return e;
     kernel<<<grid, kAdamwThreads, bytes, stream>>>(a, mask, warp_bytes);
     return cudaGetLastError();

@@ -19,6 +19,7 @@
 
 #include <type_traits>
 
+#include "launch.cuh"
 #include "peri_norm.cuh"
 
 namespace mtdao {
@@ -220,6 +221,7 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
     };
 
     if constexpr (C > 1) cooperative_groups::this_cluster().sync();   // every block of the cluster runs
+    cudaTriggerProgrammaticLaunchCompletion();         // the sums' kernel may take the places that come free
     float2 next_sf, next_sy;
     auto ask_stats = [&](int64_t n) {
         const int64_t r = first + n * step;
@@ -390,6 +392,7 @@ __global__ void __launch_bounds__(1024) peri_backward_sums_kernel(const NormArgs
     const int64_t rows = kind != kGateRows ? blocks : split ? workers + a.gate_rows : workers;
     const float *Ds = Ss + rows * a.d;
     float v[4] = {};                                   // of dh n_y, dh, dz n_f, dz
+    cudaGridDependencySynchronize();                   // launched early, see launch.cuh
     auto add = [&](const float *p, const float *q, int64_t count, float &x, float &y) {
 #pragma unroll 8
         for (int64_t k = part; k < count; k += kParts) {
@@ -456,7 +459,8 @@ cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaS
     auto kernel = KIND == kFull || (KIND == kEither && p.full) ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain>
                                                                : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull>;
     if (kBytes > 40 * 1024) {                          // with the static part, over what needs no asking
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        static std::atomic<uint64_t> done[2];
+        const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kBytes, done[p.full]);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t config = {};
@@ -518,8 +522,8 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
         }
         if (e != cudaSuccess) return e;
     }
-    peri_backward_sums_kernel<S><<<(a.d + 31) / 32, 1024, 0, stream>>>(a, p.blocks, workers, a.layer || a.post_b.p);
-    return cudaGetLastError();
+    return launch_early(peri_backward_sums_kernel<S>, dim3((a.d + 31) / 32), 1024, 0, stream, a, p.blocks, workers,
+                        a.layer || a.post_b.p);
 }
 
 }  // namespace mtdao
