@@ -6,155 +6,200 @@
 namespace mtdao {
 namespace {
 
-// The sum over a row's L lanes (W = 1) or W warps, the same in each of its threads.  parts: W floats of the
-// row's, not read by anyone since the last barrier but one.
-template <int W, int L>
-__device__ __forceinline__ float row_sum(float v, float *parts) {
+// The sums of R rows' values over L lanes (W = 1) or W warps, the same in each of the row's threads, with one
+// barrier.  parts: not read by anyone since the last barrier but one.
+template <int W, int L, int R>
+__device__ __forceinline__ void row_sums(float (&v)[R], float (&parts)[R][W]) {
 #pragma unroll
-    for (int off = L / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    if constexpr (W == 1) return v;
-    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float t = 0.0f;
+    for (int n = 0; n < R; ++n)
 #pragma unroll
-    for (int i = 0; i < W; ++i) t += parts[i];
-    return t;
+        for (int off = L / 2; off > 0; off >>= 1) v[n] += __shfl_xor_sync(0xffffffffu, v[n], off);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int n = 0; n < R; ++n) parts[n][threadIdx.x >> 5] = v[n];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < R; ++n) {
+            v[n] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[n] += parts[n][i];
+        }
+    }
 }
 
-// Rows of up to 8 V columns a thread, over L lanes (W = 1: d <= 64 and 128 take 8 and 16, 21 -> 92 %
-// of the memory's rate at d = 64) or W warps; a thread block holds one row (W > 1) or 128 / L.
-// A row's loads go out together and the row stays in registers: it is read and written once.  The
-// weights come from the first-level cache each time: a thread has no room for its columns' (up to five
-// vectors) beside the row.  (Asynchronous copies to shared memory, one to four rows ahead, were slower, 50 to 80 % of the
-// memory's rate against 78 to 91: they leave the first-level cache no room for the weights.)
-template <typename S, typename B, int V, int W, int L, bool VEC, bool LAYER>
+// Rows of up to 8 V columns a thread, over L lanes (W = 1) or W warps.  A thread takes R rows at a time (of few
+// columns; the weights are then read once for all of them); a thread block holds 128 / L or one such set.
+// The rows' loads go out together and the rows stay in registers: they are read and written once.  Thread
+// blocks follow one another, in the order of the rows; ones that stay and have the weights in registers and the next
+// rows on their way to shared memory were slower (50 to 89 % of the memory's rate against 78 to 97, d = 512 to 4096).  The
+// weights come from the first-level cache each time.  ELEMENT: a gate for every element, read with the rows.
+template <typename S, typename B, int V, int W, int L, int R, bool VEC, bool LAYER, bool ELEMENT>
 __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) peri_forward_kernel(const NormArgs a) {
-    __shared__ float parts[4][W];
-    constexpr int kThreads = W == 1 ? L : 32 * W, kRows = W == 1 ? 128 / L : 1;
+    __shared__ float parts[4][R][W];
+    constexpr int kThreads = W == 1 ? L : 32 * W, kSets = W == 1 ? 128 / L : 1, kRows = kSets * R;
     const Columns<VEC> cols{static_cast<int>(threadIdx.x) % kThreads, kThreads, a.d};
     const float inv_d = 1.0f / static_cast<float>(a.d);
     // a warp's lanes stay together: rows past the last are worked on as zeros, and not written
     const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * kRows; base < a.rows; base += step) {
-        const int64_t r = base + threadIdx.x / kThreads;
-        const bool live = kRows == 1 || r < a.rows;
-        Eight<S> x[V];
-        Eight<B> f[V];
+        const int64_t first = base + threadIdx.x / kThreads;            // and kSets on, ...
+        auto row = [&](int n) { return first + n * kSets; };
+        auto live = [&](int n) { return kRows == 1 || row(n) < a.rows; };
+        Eight<S> x[R][V];
+        Eight<B> f[R][V];
+        Eight<Bf16> g16[ELEMENT ? R : 1][ELEMENT ? V : 1];
+        Eight<float> g32[ELEMENT ? R : 1][ELEMENT ? V : 1];
 #pragma unroll
-        for (int q = 0; q < V; ++q)
-            if (live) cols.load(static_cast<const B *>(a.f) + r * a.ld_f, q, f[q]); else f[q].zero();
-#pragma unroll
-        for (int q = 0; q < V; ++q)
-            if (live) cols.load(static_cast<const S *>(a.x) + r * a.ld_x, q, x[q]); else x[q].zero();
-        float y[V][8];
-        float2 sf = make_float2(0.0f, 0.0f), sy = make_float2(0.0f, 0.0f);
-        float sum = 0.0f;
-        if constexpr (LAYER) {
+        for (int n = 0; n < R; ++n)
 #pragma unroll
             for (int q = 0; q < V; ++q)
+                if (live(n)) cols.load(static_cast<const B *>(a.f) + row(n) * a.ld_f, q, f[n][q]); else f[n][q].zero();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += f[q].get(i);
-            sf.x = row_sum<W, L>(sum, parts[0]) * inv_d;
+        for (int n = 0; n < R; ++n)
+#pragma unroll
+            for (int q = 0; q < V; ++q)
+                if (live(n)) cols.load(static_cast<const S *>(a.x) + row(n) * a.ld_x, q, x[n][q]); else x[n][q].zero();
+        if constexpr (ELEMENT) {
+#pragma unroll
+            for (int n = 0; n < R; ++n)
+#pragma unroll
+                for (int q = 0; q < V; ++q)
+                    if (live(n)) {
+                        if (a.gate.bf16) cols.load(static_cast<const Bf16 *>(a.gate.p) + row(n) * a.d, q, g16[n][q]);
+                        else cols.load(static_cast<const float *>(a.gate.p) + row(n) * a.d, q, g32[n][q]);
+                    }
         }
-        sum = 0.0f;
+        Pair z[R][V][4];
+        // mean and reciprocal deviation of the rows that get(n, q, i) gives; at: parts 0 and 1, or 2 and 3
+        auto statistics = [&](auto get, float2 (&out)[R], int at) {
+float mean[R] = {}, squares[R];
+            if constexpr (LAYER) {
 #pragma unroll
-        for (int q = 0; q < V; ++q)
+                for (int n = 0; n < R; ++n) {
+                    Pair s(0.0f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float z = f[q].get(i) - sf.x;
-                if (!LAYER || cols.valid(q, i)) sum = fmaf(z, z, sum);
+                    for (int q = 0; q < V; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s = s + get(n, q, i);
+                    mean[n] = s.lo() + s.hi();
+                }
+                row_sums<W, L>(mean, parts[at]);
             }
-        sf.y = rsqrtf(fmaf(row_sum<W, L>(sum, parts[1]), inv_d, a.eps));
-        const int64_t gate = a.gate.p && live ? gate_row(a, r) : 0;
-        sum = 0.0f;
+#pragma unroll
+            for (int n = 0; n < R; ++n) {
+                mean[n] *= inv_d;
+                Pair s(0.0f);
+#pragma unroll
+                for (int q = 0; q < V; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        Pair t = get(n, q, i);
+                        if (LAYER) {
+                            t = t + Pair(-mean[n]);
+                            if (!cols.valid(q, 2 * i)) t = Pair(0.0f);
+                            else if (!VEC && !cols.valid(q, 2 * i + 1)) t = Pair(t.lo(), 0.0f);
+                        }
+                        s = fma2(t, t, s);
+                    }
+                squares[n] = s.lo() + s.hi();
+            }
+            row_sums<W, L>(squares, parts[at + 1]);
+#pragma unroll
+            for (int n = 0; n < R; ++n) out[n] = make_float2(mean[n], rsqrtf(fmaf(squares[n], inv_d, a.eps)));
+        };
+        float2 sf[R], sy[R];
+        statistics([&](int n, int q, int i) { return f[n][q].pair(i); }, sf, 0);
 #pragma unroll
         for (int q = 0; q < V; ++q) {
-            float w[8], t[8];
+            Pair w[4], b[4], gate[4];
             a.post_w.load(cols, 0, q, w);
+            if (a.post_b.p) a.post_b.load(cols, 0, q, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = (f[q].get(i) - sf.x) * sf.y * w[i];
-            if (a.post_b.p) {
-                a.post_b.load(cols, 0, q, w);
+            for (int n = 0; n < R; ++n) {
+                if (!ELEMENT && a.gate.p && (n == 0 || a.gate_rows > 1))
+                    a.gate.load(cols, live(n) ? gate_row(a, row(n)) : 0, q, gate);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[i] += w[i];
+                for (int i = 0; i < 4; ++i) {
+                    Pair t = LAYER ? f[n][q].pair(i) + Pair(-sf[n].x) : f[n][q].pair(i);
+                    t = t * Pair(sf[n].y) * w[i];
+                    if (a.post_b.p) t = t + b[i];
+                    if (ELEMENT) t = t * (a.gate.bf16 ? g16[ELEMENT ? n : 0][ELEMENT ? q : 0].pair(i) : g32[ELEMENT ? n : 0][ELEMENT ? q : 0].pair(i));
+                    else if (a.gate.p) t = t * gate[i];
+                    z[n][q][i] = fma2(Pair(a.residual_scale), x[n][q].pair(i), t);
+                }
+                if (live(n)) cols.store(static_cast<S *>(a.y) + row(n) * a.ld_y, q, z[n][q]);
             }
-            if (a.gate.p) {
-                a.gate.load(cols, gate, q, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) t[i] *= w[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[q][i] = fmaf(a.residual_scale, x[q].get(i), t[i]);
-                if (LAYER) sum += y[q][i];
-            }
-            if (live) cols.store(static_cast<S *>(a.y) + r * a.ld_y, q, y[q]);
         }
-        if constexpr (LAYER) sy.x = row_sum<W, L>(sum, parts[2]) * inv_d;
-        sum = 0.0f;
-#pragma unroll
-        for (int q = 0; q < V; ++q)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float z = y[q][i] - sy.x;
-                if (!LAYER || cols.valid(q, i)) sum = fmaf(z, z, sum);
-            }
-        sy.y = rsqrtf(fmaf(row_sum<W, L>(sum, parts[3]), inv_d, a.eps));
+        statistics([&](int n, int q, int i) { return z[n][q][i]; }, sy, 2);
 #pragma unroll
         for (int q = 0; q < V; ++q) {
-            float w[8], h[8];
+            Pair w[4], b[4], h[4];
             a.pre_w.load(cols, 0, q, w);
+            if (a.pre_b.p) a.pre_b.load(cols, 0, q, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = (y[q][i] - sy.x) * sy.y * w[i];
-            if (a.pre_b.p) {
-                a.pre_b.load(cols, 0, q, w);
+            for (int n = 0; n < R; ++n) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[i] += w[i];
+                for (int i = 0; i < 4; ++i) {
+                    h[i] = LAYER ? z[n][q][i] + Pair(-sy[n].x) : z[n][q][i];
+                    h[i] = h[i] * Pair(sy[n].y) * w[i];
+                    if (a.pre_b.p) h[i] = h[i] + b[i];
+                }
+                if (live(n)) cols.store(static_cast<B *>(a.h) + row(n) * a.ld_h, q, h);
             }
-            if (live) cols.store(static_cast<B *>(a.h) + r * a.ld_h, q, h);
         }
-        if (a.stats && live && cols.t == 0) {
-            a.stats[r] = sf;
-            a.stats[a.rows + r] = sy;
-        }
+#pragma unroll
+        for (int n = 0; n < R; ++n)
+            if (a.stats && live(n) && cols.t == 0) {
+                a.stats[row(n)] = sf[n];
+                a.stats[a.rows + row(n)] = sy[n];
+            }
         if (W > 1) __syncthreads();                    // the next row writes parts again
     }
 }
 
-template <typename S, typename B, int V, int W, int L, bool VEC>
+template <typename S, typename B, int V, int W, int L, int R, bool VEC>
 cudaError_t launch_forward_rows(const NormArgs &a, cudaStream_t stream) {
-    constexpr int kRows = W == 1 ? 128 / L : 1;
+    constexpr int kRows = (W == 1 ? 128 / L : 1) * R;
     const int64_t blocks = (a.rows + kRows - 1) / kRows;
     const unsigned grid = static_cast<unsigned>(blocks < 0x7fffffff ? blocks : 0x7fffffff);
-    auto kernel = a.layer ? peri_forward_kernel<S, B, V, W, L, VEC, true> : peri_forward_kernel<S, B, V, W, L, VEC, false>;
+    const bool element = gate_kind(a) == kGateElement;
+    auto kernel = element ? (a.layer ? peri_forward_kernel<S, B, V, W, L, R, VEC, true, true> : peri_forward_kernel<S, B, V, W, L, R, VEC, false, true>)
+                          : (a.layer ? peri_forward_kernel<S, B, V, W, L, R, VEC, true, false> : peri_forward_kernel<S, B, V, W, L, R, VEC, false, false>);
     kernel<<<grid, W == 1 ? 128 : 32 * W, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-// As few warps as hold a row at four groups of eight columns a thread: more threads a row wait for one
-// another more (d = 2048, bf16: four groups 6050 GB/s, two 5151, one 4143).
+// A thread's columns and rows: enough of them that their loads keep the memory busy and that a weight is used for
+// two rows, few enough that three or four thread blocks' registers fit an SM.
 template <typename S, typename B>
 cudaError_t launch_peri_forward(const NormArgs &a, bool vec, cudaStream_t stream) {
     const int groups = (a.d + 255) / 256;              // of a warp's 256 columns
     if (!vec) {
-        if (groups <= 1) return launch_forward_rows<S, B, 1, 1, 32, false>(a, stream);
-        if (groups <= 4) return launch_forward_rows<S, B, 4, 1, 32, false>(a, stream);
-        if (groups <= 16) return launch_forward_rows<S, B, 4, 4, 32, false>(a, stream);
-        return launch_forward_rows<S, B, 4, 16, 32, false>(a, stream);
+        if (groups <= 1) return launch_forward_rows<S, B, 1, 1, 32, 1, false>(a, stream);
+        if (groups <= 4) return launch_forward_rows<S, B, 4, 1, 32, 1, false>(a, stream);
+        if (groups <= 16) return launch_forward_rows<S, B, 4, 4, 32, 1, false>(a, stream);
+        return launch_forward_rows<S, B, 4, 16, 32, 1, false>(a, stream);
     }
-    if (a.d <= 64) return launch_forward_rows<S, B, 1, 1, 8, true>(a, stream);
-    if (a.d <= 128) return launch_forward_rows<S, B, 1, 1, 16, true>(a, stream);
-    if (groups <= 1) return launch_forward_rows<S, B, 1, 1, 32, true>(a, stream);
-    if (groups <= 2) return launch_forward_rows<S, B, 2, 1, 32, true>(a, stream);
-    if (groups <= 3) return launch_forward_rows<S, B, 3, 1, 32, true>(a, stream);
-    if (groups <= 4) return launch_forward_rows<S, B, 4, 1, 32, true>(a, stream);
-    if (groups <= 6) return launch_forward_rows<S, B, 3, 2, 32, true>(a, stream);
-    if (groups <= 8) return launch_forward_rows<S, B, 4, 2, 32, true>(a, stream);
-    if (groups <= 16) return launch_forward_rows<S, B, 4, 4, 32, true>(a, stream);
-    if (groups <= 32) return launch_forward_rows<S, B, 4, 8, 32, true>(a, stream);
-    return launch_forward_rows<S, B, 4, 16, 32, true>(a, stream);
+    // GB/s on rows of 512 MB and more, bf16 | fp32 stream, bf16 branch | fp32; a shape by V W R:
+    //  768: 312 6226 5371 5184, 134 4841 5392 6205    1536: 322 6250 5228 4955, 232 4787 5493 5797
+    // 4096: 441 5565 4949 5227, 282 4596 5392 5680    8192: 481 5135 4294 4753, 2(16)2 4354 4685 4848
+    // and one row a thread where two or four now are: 5235 at 768, 3587 at 256, 3682 at 64 (bf16).
+    constexpr bool kWide = sizeof(S) == 4, kWider = sizeof(B) == 4;
+    if (a.d <= 64) return launch_forward_rows<S, B, 1, 1, 8, 4, true>(a, stream);
+    if (a.d <= 128) return launch_forward_rows<S, B, 1, 1, 16, 4, true>(a, stream);
+    if (groups <= 1) return launch_forward_rows<S, B, 1, 1, 32, 4, true>(a, stream);
+    if (groups <= 2) return launch_forward_rows<S, B, 2, 1, 32, 2, true>(a, stream);
+    if (groups <= 3) return launch_forward_rows<S, B, kWider ? 1 : 3, kWider ? 3 : 1, 32, kWider ? 4 : 2, true>(a, stream);
+    if (groups <= 4) return launch_forward_rows<S, B, 2, 2, 32, 2, true>(a, stream);
+    if (groups <= 6) return launch_forward_rows<S, B, kWide ? 2 : 3, kWide ? 3 : 2, 32, 2, true>(a, stream);
+    if (groups <= 8) return launch_forward_rows<S, B, 2, 4, 32, 2, true>(a, stream);
+    if (groups <= 16) return launch_forward_rows<S, B, kWide ? 2 : 4, kWide ? 8 : 4, 32, kWide ? 2 : 1, true>(a, stream);
+    if (groups <= 32) return launch_forward_rows<S, B, kWide ? 2 : 4, kWide ? 16 : 8, 32, kWide ? 2 : 1, true>(a, stream);
+    return launch_forward_rows<S, B, 4, 16, 32, 1, true>(a, stream);
 }
 
 }  // namespace mtdao
