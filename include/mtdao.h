@@ -532,13 +532,18 @@ typedef struct mtdao_adamw_ctx *mtdao_adamw_handle;
  * numel[k] >= 0 elements (one at least not empty).  decay[k] multiplies the
  * step's weight decay for tensor k (0 for norm weights and biases, say); NULL:
  * 1 for every tensor.  m = v = 0, t = 0.  The handle works on cuda_stream and
- * on the device that is current; the call synchronises that stream.
- * Errors: MTDAO_ERR_INVALID, MTDAO_ERR_OOM, MTDAO_ERR_CUDA.
+ * on the device that is current.  memory: NULL (the handle allocates what it
+ * needs and frees it), or device memory of the caller's, 256-byte aligned, of
+ * mtdao_adamw_memory bytes, which holds the states and the handle's tables until the handle is destroyed.
+ * Errors: MTDAO_ERR_INVALID, MTDAO_ERR_ALIGN, MTDAO_ERR_OOM, MTDAO_ERR_CUDA.
  */
 int mtdao_adamw_create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay,
-                       int32_t n_tensors, void *cuda_stream, mtdao_adamw_handle *out);
+                       int32_t n_tensors, void *memory, void *cuda_stream, mtdao_adamw_handle *out);
 
-/* Waits for the handle's stream and frees what the handle owns; NULL is allowed. */
+/* Bytes of device memory that such a handle needs; -1 for arguments that mtdao_adamw_create refuses.  Host-only. */
+int64_t mtdao_adamw_memory(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, int32_t n_tensors);
+
+/* Waits for the handle's stream and frees what the handle allocated; NULL is allowed. */
 void mtdao_adamw_destroy(mtdao_adamw_handle h);
 
 int mtdao_adamw_set_stream(mtdao_adamw_handle h, void *cuda_stream);

@@ -144,7 +144,9 @@ def _load():
         "mtdao_last_error": (ctypes.c_char_p, [H]),
         "mtdao_adamw_create": (ctypes.c_int, [ctypes.POINTER(mtdao_adamw_config), ctypes.c_int32, i64p,
                                               ctypes.POINTER(ctypes.c_float), ctypes.c_int32, ctypes.c_void_p,
-                                              ctypes.POINTER(H)]),
+                                              ctypes.c_void_p, ctypes.POINTER(H)]),
+        "mtdao_adamw_memory": (ctypes.c_int64, [ctypes.POINTER(mtdao_adamw_config), ctypes.c_int32, i64p,
+                                                ctypes.c_int32]),
         "mtdao_adamw_destroy": (None, [H]),
         "mtdao_adamw_set_stream": (ctypes.c_int, [H, ctypes.c_void_p]),
         "mtdao_adamw_bind_params": (ctypes.c_int, [H, ctypes.POINTER(ctypes.c_void_p),
@@ -394,12 +396,21 @@ def _check_adamw(rc, h):
     return rc
 
 
-def mtdao_adamw_create(cfg: mtdao_adamw_config, M: int, numels, decay=None, stream: int = 0):
+def mtdao_adamw_memory(cfg: mtdao_adamw_config, M: int, numels) -> int:
+    n = int(lib.mtdao_adamw_memory(ctypes.byref(cfg), M, (ctypes.c_int64 * len(numels))(*[int(k) for k in numels]),
+                                   len(numels)))
+    if n < 0:
+        _check(ERR_INVALID)
+    return n
+
+
+def mtdao_adamw_create(cfg: mtdao_adamw_config, M: int, numels, decay=None, stream: int = 0, memory: int = 0):
     n = len(numels)
     arr = (ctypes.c_int64 * n)(*[int(k) for k in numels])
     dec = None if decay is None else (ctypes.c_float * n)(*[float(k) for k in decay])
     h = ctypes.c_void_p()
-    _check(lib.mtdao_adamw_create(ctypes.byref(cfg), M, arr, dec, n, ctypes.c_void_p(stream), ctypes.byref(h)))
+    _check(lib.mtdao_adamw_create(ctypes.byref(cfg), M, arr, dec, n, ctypes.c_void_p(memory), ctypes.c_void_p(stream),
+                                  ctypes.byref(h)))
     return h
 
 

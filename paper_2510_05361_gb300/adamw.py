@@ -25,7 +25,7 @@ class AdamW:
 
     def __init__(self, params, grads=None, *, betas=(0.9, 0.999), eps: float = 1e-8, state_bits: int = 32,
                  decay=None, seed: int = 0, stream: int | None = None):
-        self._h = None
+        self._h = self._memory = None
         params = self._nested(params, "params")
         self.M = len(params)
         self.numels = [int(t.numel()) for t in params[0]]
@@ -37,12 +37,17 @@ class AdamW:
             raise ValueError("params must be in device memory")
         self.device = first.device
         codes = self._check(params, "params")
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device).cuda_stream
+        current = torch.cuda.current_stream(self.device)
+        stream = current.cuda_stream if stream is None else int(stream)
         cfg = P.mtdao_adamw_config(float(betas[0]), float(betas[1]), float(eps), self.state_bits,
                                    int(seed) % (1 << 64))
         with torch.cuda.device(self.device):
-            self._h = P.mtdao_adamw_create(cfg, self.M, self.numels, decay, stream)
+            # torch's memory, in the order of the handle's stream
+            with torch.cuda.stream(current if stream == current.cuda_stream
+                                   else torch.cuda.ExternalStream(stream, self.device)):
+                self._memory = torch.empty((P.mtdao_adamw_memory(cfg, self.M, self.numels),), dtype=torch.uint8,
+                                           device=self.device)
+            self._h = P.mtdao_adamw_create(cfg, self.M, self.numels, decay, stream, self._memory.data_ptr())
             P.mtdao_adamw_bind_params(self._h, [t.data_ptr() for row in params for t in row], codes)
         self.params, self.grads = params, None
         if grads is not None:
@@ -57,7 +62,7 @@ class AdamW:
     def close(self) -> None:
         if self._h is not None:
             P.mtdao_adamw_destroy(self._h)
-            self._h = None
+            self._h = self._memory = None
 
     def __del__(self):
         try:
@@ -125,22 +130,18 @@ class AdamW:
     def state(self, name: str):
         """The memory of "m" or "v": [M][n_state] fp32, or in 8 bits
         ``{"codes": [M][n_state] float8, "scales": [M][n_state / 256] fp32}`` (a value is
-        its code times its block's scale).  Valid until ``close``; the views keep
-        this object."""
+        its code times its block's scale).  Steps write there until ``close``."""
         which, kind = _STATES[name]
         values, scales, n = P.mtdao_adamw_state(self.h, which)
         if self.state_bits == 32:
-            return self._view(values, (self.M, n), "<f4")
-        return {"codes": self._view(values, (self.M, n), "|u1").view(kind),
-                "scales": self._view(scales, (self.M, n // P.ADAMW_BLOCK), "<f4")}
+            return self._view(values, (self.M, n), torch.float32)
+        return {"codes": self._view(values, (self.M, n), kind),
+                "scales": self._view(scales, (self.M, n // P.ADAMW_BLOCK), torch.float32)}
 
-    def _view(self, ptr, shape, typestr):
-        class Memory:
-            def __init__(self, owner):
-                self.owner = owner
-                self.__cuda_array_interface__ = {"shape": shape, "typestr": typestr, "data": (ptr, False),
-                                                 "version": 3, "strides": None}
-        return torch.as_tensor(Memory(self), device=self.device)
+    def _view(self, ptr, shape, kind):
+        at = ptr - self._memory.data_ptr()
+        size = shape[0] * shape[1] * (4 if kind == torch.float32 else 1)
+        return self._memory[at:at + size].view(kind).view(shape)
 
     def set_stream(self, stream: int) -> None:
         P.mtdao_adamw_set_stream(self.h, stream)

@@ -880,8 +880,9 @@ cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, in
     return cudaGetLastError();
 }
 
-int32_t adamw_chunk(int num_sms, int bits, int64_t elements) {
-    return bits == 8 && elements >= static_cast<int64_t>(num_sms) * 8 * kAdamwLongChunk ? kAdamwLongChunk : kAdamwChunk;
+// Long records where there are some eight for each SM of the device this is written for.
+int32_t adamw_chunk(int bits, int64_t elements) {
+    return bits == 8 && elements >= int64_t(152) * 8 * kAdamwLongChunk ? kAdamwLongChunk : kAdamwChunk;
 }
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {

@@ -69,7 +69,7 @@ cudaError_t launch_adamw_bind(AdamwChunk *chunks, const AdamwTensor *tensors, in
                               int32_t M, cudaStream_t stream);
 
 // The record's length for a list of so many elements over all replicas.
-int32_t adamw_chunk(int num_sms, int bits, int64_t elements);
+int32_t adamw_chunk(int bits, int64_t elements);
 int32_t adamw_warp_bytes(bool grad_bf16, bool param_bf16);
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream);
 

@@ -25,7 +25,7 @@ struct mtdao_adamw_ctx {
     int32_t n_tensors = 0;
     std::vector<AdamwTensor> tensors;
     AdamwList list = {};
-    void *memory = nullptr;              // the one allocation; what follows lies in it
+    void *memory = nullptr;              // what the handle allocated itself, if it did
     AdamwChunk *chunks = nullptr;
     AdamwTensor *tensors_dev = nullptr;
     void **table = nullptr;              // [M][n_tensors], scratch of a binding
@@ -81,11 +81,19 @@ void release(mtdao_adamw_ctx *h) {
 
 bool rate(double b) { return b >= 0.0 && b < 1.0; }
 
-int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay, int32_t n_tensors,
-           void *cuda_stream, mtdao_adamw_ctx *h) {
-    h->cfg = *cfg;
-    h->n_tensors = n_tensors;
-    h->tensors.resize(n_tensors);
+// The configuration and the list, with no device.  Fills in the tensors' places and the list's sizes.
+int plan(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay, int32_t n_tensors,
+         std::vector<AdamwTensor> &tensors, AdamwList &a) {
+    if (cfg == nullptr) return set_thread_error(MTDAO_ERR_INVALID, "config is NULL");
+    if (!rate(cfg->beta1) || !rate(cfg->beta2))
+        return fail(nullptr, MTDAO_ERR_INVALID, "beta1=%g, beta2=%g must lie in [0,1)", cfg->beta1, cfg->beta2);
+    if (!(std::isfinite(cfg->eps) && cfg->eps >= 1e-15))
+        return fail(nullptr, MTDAO_ERR_INVALID, "eps=%g must be at least 1e-15", cfg->eps);
+    if (cfg->state_bits != 8 && cfg->state_bits != 32)
+        return fail(nullptr, MTDAO_ERR_INVALID, "state_bits=%d must be 8 or 32", cfg->state_bits);
+    if (M < 1 || M > MTDAO_MAX_REPLICAS)
+        return fail(nullptr, MTDAO_ERR_INVALID, "M %d outside 1..%d", M, MTDAO_MAX_REPLICAS);
+    if (numel == nullptr || n_tensors < 1) return set_thread_error(MTDAO_ERR_INVALID, "empty tensor list");
     int64_t elements = 0;
     for (int32_t k = 0; k < n_tensors; ++k) {
         if (numel[k] < 0 || numel[k] > (int64_t(1) << 40) || (elements += numel[k]) > (int64_t(1) << 40))
@@ -96,68 +104,81 @@ int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const
             return fail(nullptr, MTDAO_ERR_INVALID, "decay[%d]=%g must be finite and not negative", k, d);
     }
     if (elements == 0) return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list holds no element");
-    h->stream = static_cast<cudaStream_t>(cuda_stream);
-    int sms = 1;
-    cudaError_t e = cudaGetDevice(&h->device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
-    if (e != cudaSuccess) return cuda_fail(nullptr, e, "no usable CUDA device");
-
-    const int32_t chunk = adamw_chunk(sms, cfg->state_bits, elements * M);
+    a.M = M;
+    a.bits = cfg->state_bits;
+    a.chunk = adamw_chunk(a.bits, elements * M);
+    tensors.resize(n_tensors);
     int64_t chunks = 0, blocks = 0;
     for (int32_t k = 0; k < n_tensors; ++k) {
-        h->tensors[k] = {numel[k], chunks, blocks, decay ? decay[k] : 1.0f, 0};
-        chunks += (numel[k] + chunk - 1) / chunk;
+        tensors[k] = {numel[k], chunks, blocks, decay ? decay[k] : 1.0f, 0};
+        chunks += (numel[k] + a.chunk - 1) / a.chunk;
         blocks += (numel[k] + kAdamwBlock - 1) / kAdamwBlock;
     }
     // the records count blocks in 32 bits, a grid a replica's chunks in 31, the random numbers groups of 8 in 32
     if (blocks * M > 0xffffffffll || chunks > 0x7fffffffll || blocks * (kAdamwBlock / 8) > 0xffffffffll)
         return fail(nullptr, MTDAO_ERR_INVALID, "the tensor list is too long for %d replicas", M);
-
-    AdamwList &a = h->list;
-    a.M = M;
-    a.bits = cfg->state_bits;
     a.n_chunks = chunks;
-    a.chunk = chunk;
     a.n_state = blocks * kAdamwBlock;
-    const size_t held = static_cast<size_t>(M) * a.n_state * (a.bits / 8);
-    const size_t scales = a.bits == 8 ? static_cast<size_t>(M) * blocks * sizeof(float) : 0;
+    return MTDAO_OK;
+}
+
+// What a handle holds on the device, in one piece; sets the addresses where there is one, and gives its size.
+size_t place(const AdamwList &sizes, int32_t n_tensors, char *memory, AdamwList &a, mtdao_adamw_ctx *h) {
+    const size_t M = sizes.M, held = M * sizes.n_state * (sizes.bits / 8);
+    const size_t scales = sizes.bits == 8 ? M * (sizes.n_state / kAdamwBlock) * sizeof(float) : 0;
+    void *none = nullptr;
     struct {
         void **p;
         size_t bytes;
-    } allocs[] = {
+    } parts[] = {
         {&a.m, held},
         {&a.v, held},
         {reinterpret_cast<void **>(&a.m_scale), scales},
         {reinterpret_cast<void **>(&a.v_scale), scales},
-        {reinterpret_cast<void **>(&h->chunks), static_cast<size_t>(M) * chunks * sizeof(AdamwChunk)},
-        {reinterpret_cast<void **>(&h->tensors_dev), n_tensors * sizeof(AdamwTensor)},
-        {reinterpret_cast<void **>(&h->table), static_cast<size_t>(M) * n_tensors * sizeof(void *)},
-        {reinterpret_cast<void **>(&h->dtypes), n_tensors * sizeof(int32_t)},
-        {reinterpret_cast<void **>(&h->norm_partial), static_cast<size_t>(adamw_norm_partials(a)) * sizeof(double)},
-        {reinterpret_cast<void **>(&h->norm_arrived), M * sizeof(uint32_t)},
-        {reinterpret_cast<void **>(&h->clip_scale), M * sizeof(float)},
+        {h ? reinterpret_cast<void **>(&h->chunks) : &none, M * sizes.n_chunks * sizeof(AdamwChunk)},
+        {h ? reinterpret_cast<void **>(&h->tensors_dev) : &none, n_tensors * sizeof(AdamwTensor)},
+        {h ? reinterpret_cast<void **>(&h->table) : &none, M * n_tensors * sizeof(void *)},
+        {h ? reinterpret_cast<void **>(&h->dtypes) : &none, n_tensors * sizeof(int32_t)},
+        {h ? reinterpret_cast<void **>(&h->norm_partial) : &none, adamw_norm_partials(sizes) * sizeof(double)},
+        {h ? reinterpret_cast<void **>(&h->norm_arrived) : &none, M * sizeof(uint32_t)},
+        {h ? reinterpret_cast<void **>(&h->clip_scale) : &none, M * sizeof(float)},
     };
-    // one allocation: a call to the driver costs more than setting up a small list
-    size_t total = 0;
-    for (auto &x : allocs) total += (x.bytes + 255) / 256 * 256;
-    e = cudaMalloc(&h->memory, total);
-    if (e != cudaSuccess) {
-        cudaGetLastError();
-        h->memory = nullptr;
-        return fail(nullptr, MTDAO_ERR_OOM, "cudaMalloc of states and tables (%zu bytes) failed: %s", total,
-                    cudaGetErrorString(e));
-    }
     size_t at = 0;
-    for (auto &x : allocs) {
-        if (x.bytes) *x.p = static_cast<char *>(h->memory) + at;
+    for (auto &x : parts) {
+        if (memory && x.bytes) *x.p = memory + at;
         at += (x.bytes + 255) / 256 * 256;
     }
+    return at;
+}
+
+int create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay, int32_t n_tensors,
+           void *memory, void *cuda_stream, mtdao_adamw_ctx *h) {
+    AdamwList &a = h->list;
+    if (int rc = plan(cfg, M, numel, decay, n_tensors, h->tensors, a)) return rc;
+    if (reinterpret_cast<uintptr_t>(memory) % 256)
+        return set_thread_error(MTDAO_ERR_ALIGN, "memory is not 256-byte aligned");
+    h->cfg = *cfg;
+    h->n_tensors = n_tensors;
+    h->stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = cudaGetDevice(&h->device);
+    if (e != cudaSuccess) return cuda_fail(nullptr, e, "no usable CUDA device");
+    const size_t total = place(a, n_tensors, nullptr, a, h);
+    if (memory == nullptr) {
+        e = cudaMalloc(&h->memory, total);
+        if (e != cudaSuccess) {
+            h->memory = nullptr;
+            cudaGetLastError();
+            return fail(nullptr, MTDAO_ERR_OOM, "cudaMalloc of states and tables (%zu bytes) failed: %s", total,
+                        cudaGetErrorString(e));
+        }
+        memory = h->memory;
+    }
+    place(a, n_tensors, static_cast<char *>(memory), a, h);
     a.chunks = h->chunks;
-    e = cudaMemsetAsync(h->memory, 0, total, h->stream);
-    if (e == cudaSuccess)
+    e = cudaMemsetAsync(memory, 0, total, h->stream);
+    if (e == cudaSuccess)                               // from memory that is not pinned: read before the call returns
         e = cudaMemcpyAsync(h->tensors_dev, h->tensors.data(), n_tensors * sizeof(AdamwTensor), cudaMemcpyHostToDevice,
                             h->stream);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(h->stream);
     return e == cudaSuccess ? MTDAO_OK : cuda_fail(nullptr, e, "setting up the states");
 }
 
@@ -207,34 +228,36 @@ int no_handle() { return set_thread_error(MTDAO_ERR_INVALID, "handle is NULL"); 
 }  // namespace
 
 extern "C" int mtdao_adamw_create(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, const float *decay,
-                                  int32_t n_tensors, void *cuda_stream, mtdao_adamw_handle *out) {
+                                  int32_t n_tensors, void *memory, void *cuda_stream, mtdao_adamw_handle *out) {
     if (out == nullptr) return set_thread_error(MTDAO_ERR_INVALID, "out is NULL");
     *out = nullptr;
-    if (cfg == nullptr) return set_thread_error(MTDAO_ERR_INVALID, "config is NULL");
-    if (!rate(cfg->beta1) || !rate(cfg->beta2))
-        return fail(nullptr, MTDAO_ERR_INVALID, "beta1=%g, beta2=%g must lie in [0,1)", cfg->beta1, cfg->beta2);
-    if (!(std::isfinite(cfg->eps) && cfg->eps >= 1e-15))
-        return fail(nullptr, MTDAO_ERR_INVALID, "eps=%g must be at least 1e-15", cfg->eps);
-    if (cfg->state_bits != 8 && cfg->state_bits != 32)
-        return fail(nullptr, MTDAO_ERR_INVALID, "state_bits=%d must be 8 or 32", cfg->state_bits);
-    if (M < 1 || M > MTDAO_MAX_REPLICAS)
-        return fail(nullptr, MTDAO_ERR_INVALID, "M %d outside 1..%d", M, MTDAO_MAX_REPLICAS);
-    if (numel == nullptr || n_tensors < 1) return set_thread_error(MTDAO_ERR_INVALID, "empty tensor list");
     mtdao_adamw_ctx *h = nullptr;
     int rc;
     try {
         h = new mtdao_adamw_ctx();
-        rc = create(cfg, M, numel, decay, n_tensors, cuda_stream, h);
+        rc = create(cfg, M, numel, decay, n_tensors, memory, cuda_stream, h);
     } catch (const std::bad_alloc &) {
         rc = set_thread_error(MTDAO_ERR_OOM, "out of host memory");
     }
     if (rc == MTDAO_OK) {
         *out = h;
     } else if (h != nullptr) {
-        release(h);
+        if (h->memory) release(h);
         delete h;
     }
     return rc;
+}
+
+extern "C" int64_t mtdao_adamw_memory(const mtdao_adamw_config *cfg, int32_t M, const int64_t *numel, int32_t n_tensors) {
+    try {
+        std::vector<AdamwTensor> tensors;
+        AdamwList a = {};
+        if (plan(cfg, M, numel, nullptr, n_tensors, tensors, a)) return -1;
+        return static_cast<int64_t>(place(a, n_tensors, nullptr, a, nullptr));
+    } catch (const std::bad_alloc &) {
+        set_thread_error(MTDAO_ERR_OOM, "out of host memory");
+        return -1;
+    }
 }
 
 extern "C" void mtdao_adamw_destroy(mtdao_adamw_handle h) {
