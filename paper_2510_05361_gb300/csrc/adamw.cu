@@ -189,22 +189,31 @@ __device__ __forceinline__ void load_block(const AdamwList &a, const AdamwChunk 
     turn_raw(c.flags & kAdamwParamBf16, p_whole, stage, r.p);
 }
 
-// FAST: bf16 parameters and gradients, aligned, a full block.
+// What a kernel knows of the list's tensors: bf16 or not (0, 1; 2: a record's flags say it), gradients and
+// parameters, and whether all of them are aligned.
+template <int G16, int P16, bool ALIGNED>
+struct Kind {
+    static constexpr bool kAligned = ALIGNED, kOne = G16 != 2;         // kOne: one kind of tensor only
+    static __device__ __forceinline__ bool g16(const AdamwChunk &c) { return G16 == 2 ? (c.flags & kAdamwGradBf16) != 0 : G16 == 1; }
+    static __device__ __forceinline__ bool p16(const AdamwChunk &c) { return P16 == 2 ? (c.flags & kAdamwParamBf16) != 0 : P16 == 1; }
+};
+using AnyKind = Kind<2, 2, false>;
+
 // In 8 bits m and v are formed with a rounding after each operation: what the formula
 // gives then does not depend on a compiler's choice of fused operations, and a test can ask
 // for its very codes.  beta multiplies the block's scale, a power of two, rather than
 // each value.  The square root and the reciprocal are the hardware's (2^-22 together): their error is
 // far below what p's own rounding leaves.
-template <int BITS, bool CLIP, bool FAST>
+template <int BITS, bool CLIP, typename K, bool FULL>
 __device__ __forceinline__ void update_block(const AdamwList &a, const AdamwScalars &sc, const AdamwChunk &c, uint32_t replica,
                                              float s, int warp, uint32_t *stage, Raw<BITS> &r) {
     const int lane = threadIdx.x & 31, at = warp * kAdamwBlock + 8 * lane;
     const uint32_t block = c.block + warp;
     const int64_t eight = static_cast<int64_t>(block) * (kAdamwBlock / 8) + lane;
-    const bool p16 = FAST || (c.flags & kAdamwParamBf16);
+    const bool p16 = K::p16(c);
     const float keep = fmaf(-sc.decay, c.decay, 1.0f);
     Pair g[4], p[4];
-    to_pairs(r.g, FAST || (c.flags & kAdamwGradBf16), g);
+    to_pairs(r.g, K::g16(c), g);
     to_pairs(r.p, p16, p);
     if constexpr (BITS == 8) {
         decode_m(r.cm, sc.b1 * r.scale_m, r.m);
@@ -242,7 +251,7 @@ __device__ __forceinline__ void update_block(const AdamwList &a, const AdamwScal
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(i & 1 ? p[i / 2].hi() : p[i / 2].lo());
     }
-    const bool whole = FAST || ((warp + 1) * kAdamwBlock <= c.n && (c.flags & kAdamwParamAligned));
+    const bool whole = (FULL || (warp + 1) * kAdamwBlock <= c.n) && (K::kAligned || (c.flags & kAdamwParamAligned));
     store_raw(c.p, p16, whole, at, c.n, stage, w);
     if constexpr (BITS == 8) {
         float scale_m, scale_v;
@@ -330,17 +339,17 @@ __device__ __forceinline__ float clip_factor(const float *clip) {
 }
 
 // A warp's blocks first, first + 8, ... below end of a record, as many on their way at a time as fit
-// into its part of shared memory.  BF16: bf16 parameters and gradients, aligned: all four.
-template <bool CLIP, bool BF16>
+// into its part of shared memory: all four where the list has one kind of tensors.
+template <bool CLIP, typename K>
 __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwScalars &sc, const AdamwChunk &c, uint32_t replica,
                                               const float *clip, int first, int end, char *mine) {
     constexpr int kWarps = kAdamwThreads / 32;
     const int lane = threadIdx.x & 31;
-    const bool g16 = BF16 || (c.flags & kAdamwGradBf16), p16 = BF16 || (c.flags & kAdamwParamBf16);
-    const int g_skew = BF16 ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.g) & 15);
-    const int p_skew = BF16 ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.p) & 15);
+    const bool g16 = K::g16(c), p16 = K::p16(c);
+    const int g_skew = K::kAligned ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.g) & 15);
+    const int p_skew = K::kAligned ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(c.p) & 15);
     const int p_at = tensor_bytes(g16), codes_at = p_at + tensor_bytes(p16), slot = slot_bytes(g16, p16);
-    const int fit = BF16 ? kAhead : min(kAhead, a.warp_bytes / slot);
+    const int fit = K::kOne ? kAhead : min(kAhead, a.warp_bytes / slot);
     float s = 1.0f, scales = 0.0f;
     if (lane < 2 * kAhead) {
         const int b = first + (lane >> 1) * kWarps;
@@ -358,7 +367,7 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
         copies_commit();
     };
     auto work = [&](int i, char *at) {
-        if (!BF16) __syncwarp();                       // a lane reads what its neighbours copied
+        if (!K::kAligned || !g16 || !p16) __syncwarp();  // a lane reads what its neighbours copied
         Raw<8> r;
         read_elements(at, g16, g_skew, r.g);
         read_elements(at + p_at, p16, p_skew, r.p);
@@ -367,9 +376,9 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
         r.scale_m = __shfl_sync(0xffffffffu, scales, 2 * i);
         r.scale_v = __shfl_sync(0xffffffffu, scales, 2 * i + 1);
         // (an exchange takes place where the block's elements came in)
-        update_block<8, CLIP, BF16>(a, sc, c, replica, s, first + i * kWarps, reinterpret_cast<uint32_t *>(at), r);
+        update_block<8, CLIP, K, true>(a, sc, c, replica, s, first + i * kWarps, reinterpret_cast<uint32_t *>(at), r);
     };
-    if constexpr (BF16) {
+    if constexpr (K::kOne) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fetch(i, mine + i * slot);
         s = clip_factor<CLIP>(clip);
@@ -401,10 +410,10 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
     }
 }
 
-// BF16: all of the list's tensors are bf16, parameters and gradients, and aligned.  (Apart, because
-// the code for every case needs more registers: 6065 against 6549 GB/s on 2^27 bf16 elements.)
-template <int BITS, bool CLIP, bool BF16>
-__global__ void __launch_bounds__(kAdamwThreads, BITS == 32 || BF16 ? 4 : 3)
+// A kernel for each kind of list: with a record's flags deciding (as for lists of several kinds, or in 32 bits, where it
+// costs nothing) 2^27 elements in 8 bits took 222 us for 206 in bf16, 389 for 283 where misaligned, 357 for 310 in fp32.  As many thread blocks an SM as shared memory holds, in 32 bits and bf16 four.
+template <int BITS, bool CLIP, typename K, int BLOCKS>
+__global__ void __launch_bounds__(kAdamwThreads, BLOCKS)
     adamw_step_kernel(const AdamwList a, const AdamwScalars sc, const float *clip_scale) {
     constexpr int kWarps = kAdamwThreads / 32;
     constexpr uint32_t kAligned = kAdamwParamAligned | kAdamwGradAligned;
@@ -418,17 +427,17 @@ __global__ void __launch_bounds__(kAdamwThreads, BITS == 32 || BF16 ? 4 : 3)
     if constexpr (BITS == 8) {
         // a misaligned tensor's outermost granules hold bytes beside it: its first block, and one with
         // less than a granule of the tensor behind it, are read element by element
-        const bool aligned = BF16 || (c.flags & kAligned) == kAligned;
+        const bool aligned = K::kAligned || (c.flags & kAligned) == kAligned;
         lo = aligned || !(c.flags & kAdamwFirst) ? 0 : 1;
         hi = (aligned || !(c.flags & kAdamwLast) ? c.n : c.n - 8) / kAdamwBlock;
         const int from = first < lo ? first + kWarps : first;
-        if (from < hi) stream_blocks<CLIP, BF16>(a, sc, c, replica, s, from, hi, mine);
+        if (from < hi) stream_blocks<CLIP, K>(a, sc, c, replica, s, from, hi, mine);
     }
     for (int b = first; b * kAdamwBlock < c.n; b += kWarps) {
         if (b >= lo && b < hi) continue;
         Raw<BITS> r;
         load_block<BITS>(a, c, b, reinterpret_cast<uint32_t *>(mine), r);
-        update_block<BITS, CLIP, false>(a, sc, c, replica, clip_factor<CLIP>(s), b, reinterpret_cast<uint32_t *>(mine), r);
+        update_block<BITS, CLIP, AnyKind, false>(a, sc, c, replica, clip_factor<CLIP>(s), b, reinterpret_cast<uint32_t *>(mine), r);
     }
 }
 
@@ -887,18 +896,33 @@ int32_t adamw_chunk(int bits, int64_t elements) {
 
 cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const float *clip_scale, cudaStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.n_chunks), a.M);
+    const bool clip = clip_scale != nullptr;
     int bytes = kAdamwThreads / 32 * kStageBytes;
-    auto kernel = clip_scale ? adamw_step_kernel<32, true, false> : adamw_step_kernel<32, false, false>;
+    auto kernel = clip ? adamw_step_kernel<32, true, AnyKind, 4> : adamw_step_kernel<32, false, AnyKind, 4>;
     if (a.bits == 8) {
-        kernel = a.all_bf16 ? (clip_scale ? adamw_step_kernel<8, true, true> : adamw_step_kernel<8, false, true>)
-                            : (clip_scale ? adamw_step_kernel<8, true, false> : adamw_step_kernel<8, false, false>);
+        switch (a.kind) {
+#define MTDAO_ADAMW_KIND(G16, P16, ALIGNED, BLOCKS)                                              \
+    case 4 * ALIGNED + 2 * G16 + P16:                                                            \
+        kernel = clip ? adamw_step_kernel<8, true, Kind<G16, P16, ALIGNED>, BLOCKS>              \
+                      : adamw_step_kernel<8, false, Kind<G16, P16, ALIGNED>, BLOCKS>;            \
+        break;
+            MTDAO_ADAMW_KIND(1, 1, true, 4)
+            MTDAO_ADAMW_KIND(1, 0, true, 3)
+            MTDAO_ADAMW_KIND(0, 1, true, 3)
+            MTDAO_ADAMW_KIND(0, 0, true, 2)
+            MTDAO_ADAMW_KIND(1, 1, false, 4)
+            MTDAO_ADAMW_KIND(1, 0, false, 3)
+            MTDAO_ADAMW_KIND(0, 1, false, 3)
+            MTDAO_ADAMW_KIND(0, 0, false, 2)
+#undef MTDAO_ADAMW_KIND
+            default: kernel = clip ? adamw_step_kernel<8, true, AnyKind, 3> : adamw_step_kernel<8, false, AnyKind, 3>;
+        }
         bytes = kAdamwThreads / 32 * a.warp_bytes;
-        static std::atomic<uint64_t> done[4];
-        const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kMostShared,
-                                           done[2 * (clip_scale != nullptr) + (a.all_bf16 != 0)]);
+        static std::atomic<uint64_t> done[2][kAdamwMixed + 1];
+        const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kMostShared, done[clip][a.kind]);
         if (e != cudaSuccess) return e;
     }
-    if (clip_scale) return launch_early(kernel, grid, kAdamwThreads, bytes, stream, a, sc, clip_scale);
+    if (clip) return launch_early(kernel, grid, kAdamwThreads, bytes, stream, a, sc, clip_scale);
     kernel<<<grid, kAdamwThreads, bytes, stream>>>(a, sc, clip_scale);
     return cudaGetLastError();
 }

@@ -31,6 +31,8 @@ constexpr uint32_t kAdamwParamBf16 = 1, kAdamwGradBf16 = 2;
 constexpr uint32_t kAdamwParamAligned = 4, kAdamwGradAligned = 8;
 constexpr uint32_t kAdamwFirst = 16, kAdamwLast = 32;        // of its tensor
 
+constexpr int kAdamwMixed = 8;       // tensors of several types
+
 // What does not depend on the step.
 struct AdamwList {
     const AdamwChunk *chunks;    // [M][n_chunks]
@@ -41,7 +43,7 @@ struct AdamwList {
     int32_t bits;                // 32 or 8
     int32_t warp_bytes;          // 8 bits: a warp's shared memory (adamw_warp_bytes of most of the list)
     int32_t params_bf16;         // 8 bits: most parameters are
-    int32_t all_bf16;            // 8 bits: every tensor bf16 and aligned, parameters and gradients
+    int32_t kind;                // 8 bits: 4 all aligned + 2 gradients bf16 + parameters bf16, or kAdamwMixed
     void *m, *v;                 // [M][n_state] fp32, e4m3 and e5m2 in 8 bits
     float *m_scale, *v_scale;    // [M][n_state / kAdamwBlock]
 };

@@ -323,16 +323,19 @@ extern "C" int mtdao_adamw_bind_grads(mtdao_adamw_handle h, const void *const *g
         if (int rc = upload(h, table, dtype, true)) return rc;
         // shared memory for the kind of tensor that most elements are of
         int64_t elements[2][2] = {}, most = -1;
+        int kinds = 0;
         for (int32_t k = 0; k < h->n_tensors; ++k)
             elements[dtype[k] == MTDAO_BF16][h->param_types[k] == MTDAO_BF16] += h->tensors[k].numel;
         for (int g = 0; g < 2; ++g)
-            for (int p = 0; p < 2; ++p)
-                if (elements[g][p] > most) {
-                    most = elements[g][p];
-                    h->list.warp_bytes = adamw_warp_bytes(g, p);
-                }
-        h->list.all_bf16 = elements[0][0] + elements[0][1] + elements[1][0] == 0 && h->params_aligned &&
-                           all_aligned(h, table, dtype);
+            for (int p = 0; p < 2; ++p) {
+                kinds += elements[g][p] > 0;
+                if (elements[g][p] <= most) continue;
+                most = elements[g][p];
+                h->list.warp_bytes = adamw_warp_bytes(g, p);
+                h->list.kind = 2 * g + p;
+            }
+        if (kinds > 1) h->list.kind = kAdamwMixed;
+        else if (h->params_aligned && all_aligned(h, table, dtype)) h->list.kind += 4;
         h->has_grads = true;
         return MTDAO_OK;
     } catch (const std::bad_alloc &) {
