@@ -78,7 +78,7 @@ cudaError_t launch_adamw_step(const AdamwList &a, const AdamwScalars &sc, const 
 // ||g||^2 of each replica into sums[M] (fixed order) and, where scale is not
 // NULL, min(1, max_norm / (||g|| + 1e-6)) into scale[M].  partial: adamw_norm_partials()
 // doubles; arrived: M counters, zero before and after.
-constexpr int kAdamwNormBlocks = 8192;           // over all replicas, where there are that many records
+constexpr int kAdamwNormBlocks = 608;            // over all replicas: as many as run at once on 152 SMs
 int64_t adamw_norm_partials(const AdamwList &a);
 cudaError_t launch_adamw_norm(const AdamwList &a, double *partial, uint32_t *arrived, double *sums, float *scale,
                               double max_norm, cudaStream_t stream);
