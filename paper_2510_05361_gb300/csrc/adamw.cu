@@ -763,9 +763,14 @@ __device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwCh
             __syncwarp();                              // everything is read before the place is filled again
             fetch();
         }
-        const float count = static_cast<float>(M), part = 1.0f / count;
-        const bool exact = (M & (M - 1)) == 0;         // then the product is the quotient
-        auto mean = [&](Pair x) { return exact ? x * Pair(part) : Pair(x.lo() / count, x.hi() / count); };
+        // x / M to the nearest, by Markstein's method: the product with the nearest 1 / M, corrected by its remainder.
+        // (What is not finite becomes NaN; the bf16 parameters' mean keeps its infinities.)
+        const Pair part(1.0f / static_cast<float>(M)), less(-static_cast<float>(M));
+        auto mean = [&](Pair x) {
+            const Pair q = x * part;
+            return fma2(fma2(q, less, x), part, q);
+        };
+        auto plain_mean = [&](float x) { return x / static_cast<float>(M); };
         const int64_t block = c.block + b;
         if (!P16 && (mask & 1u)) {                     // s_0 + (sum of differences) / M
             bool odd = false;
@@ -788,7 +793,8 @@ __device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwCh
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const Pair x = mean(ps[i]);
-                    w[i] = bf16_nearest2(x.lo(), x.hi());
+                    const bool odd = x.lo() != x.lo() || x.hi() != x.hi();
+                    w[i] = odd ? bf16_nearest2(plain_mean(ps[i].lo()), plain_mean(ps[i].hi())) : bf16_nearest2(x.lo(), x.hi());
                 }
             } else {
 #pragma unroll

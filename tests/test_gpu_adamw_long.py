@@ -113,3 +113,19 @@ def test_average_with_values_that_are_not_finite(P):
         rest = torch.cat([p[:5], p[9:]])
         assert (rest == 2.0).all()
     opt.close()
+
+
+def test_average_of_bf16_parameters_that_are_not_finite(P):
+    M, n = 3, 4000
+    params = [[torch.full((n,), 1.0 + r, device="cuda", dtype=torch.bfloat16)] for r in range(M)]
+    params[1][0][5] = float("inf")
+    params[0][0][6], params[2][0][6] = float("inf"), float("-inf")
+    params[2][0][7] = float("nan")
+    opt = P.AdamW(params, state_bits=8)
+    opt.average(P.adamw.PARAMS)
+    torch.cuda.synchronize()
+    for r in range(M):
+        p = params[r][0]
+        assert p[5] == float("inf") and torch.isnan(p[6]) and torch.isnan(p[7])
+        assert (p[:5] == 2.0).all() and (p[8:] == 2.0).all()
+    opt.close()
