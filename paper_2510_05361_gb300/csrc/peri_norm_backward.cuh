@@ -84,22 +84,35 @@ constexpr int kBackThreads = W == 3 ? 96 : W <= 4 ? 128 : 32 * W;
 template <int V>
 constexpr int kRowsAhead = V == 1 ? 3 : 2;
 
+constexpr int kSharedMost = 222 * 1024;                 // an SM's shared memory, but for the static parts
+
+// Shared memory for the rows on their way, and whether a gate for every element comes the same way: with eight columns
+// a thread, where there is room without a thread block less an SM.  With sixteen the registers do not last.
+template <typename S, typename B, int V, int W, bool VEC>
+constexpr int kIncoming = VEC ? kRowsAhead<V> * V * static_cast<int>(sizeof(S) + sizeof(B)) * kBackThreads<W> * 16 : 0;
+template <int V, int W>
+constexpr int kIncomingGate = kRowsAhead<V> * V * 2 * kBackThreads<W> * 16;
+template <typename S, typename B, int V, int W, bool VEC>
+constexpr bool kStageGate =
+    VEC && V == 1 && (kIncoming<S, B, V, W, VEC> + kIncomingGate<V, W>) * (512 / kBackThreads<W>) <= kSharedMost;
+
 // V groups of eight columns a thread.  FULL: "layer" norm or biases; else the sums of dh and dY and the means are
-// left out.
-template <typename S, typename B, int V, int W, int L, int C, bool VEC, bool FULL>
+// left out.  ELEMENT: a gate for every element (apart: its code costs the others the registers that they need).
+template <typename S, typename B, int V, int W, int L, int C, bool VEC, bool FULL, bool ELEMENT>
 __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_backward_kernel(const NormArgs a) {
     constexpr int kSums = FULL ? 4 : 2;                 // A, S or A, S, B, D
     constexpr int kBlock = kBackThreads<W>, kThreads = W == 1 ? L : 32 * W, G = kBlock / kThreads;
-    constexpr int kPieces = 2 * (static_cast<int>(sizeof(S)) + static_cast<int>(sizeof(B))) / 2;     // of 16 bytes, of a group of columns
+    constexpr bool kStage = ELEMENT && kStageGate<S, B, V, W, VEC>;
+    constexpr int kRows = static_cast<int>(sizeof(S) + sizeof(B)), kPieces = kRows + (kStage ? 2 : 0);   // of 16 bytes
     constexpr int kAhead = kRowsAhead<V>;
-    extern __shared__ __align__(16) char incoming[];    // [kAhead][V][kPieces][threads][16]
+    extern __shared__ __align__(16) char incoming[];    // [kAhead][V][pieces][threads][16]
     __shared__ RowSums<W, L, G, C> sums;
     const int group = threadIdx.x / kThreads;
     const int rank = C > 1 ? static_cast<int>(cooperative_groups::this_cluster().block_rank()) : 0;
     const int64_t block = blockIdx.x / C, worker = block * G + group, workers = static_cast<int64_t>(gridDim.x / C) * G;
     const Columns<VEC> cols{rank * kThreads + static_cast<int>(threadIdx.x) % kThreads, kThreads * C, a.d};
     const float inv_d = 1.0f / static_cast<float>(a.d);
-    const int kind = gate_kind(a);
+    const int kind = ELEMENT ? static_cast<int>(kGateElement) : gate_kind(a);
 
     // a worker's rows: first, first + step, ... below end.  The workers of one warp go through as many rounds.
     int64_t first = worker, end = a.rows, step = workers, rounds = (a.rows - block * G + workers - 1) / workers;
@@ -138,7 +151,7 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
     constexpr int kB = sizeof(B) / 2, kS = sizeof(S) / 2, kLanes = W == 1 ? L : 32;
     const int lane = static_cast<int>(threadIdx.x) % kLanes;
     auto region = [&](int buffer, int q, int n) {
-        const int p = n == 0 ? 0 : n == 1 ? kB : n == 2 ? kB + kS : kB + 2 * kS;
+        const int p = n == 0 ? 0 : n == 1 ? kB : n == 2 ? kB + kS : n == 3 ? kB + 2 * kS : kRows;      // 4: the gate
         return incoming + ((buffer * V + q) * kPieces + p) * kBlock * 16;
     };
     auto copy = [&](auto *row, int64_t ld, int64_t r, int buffer, int n) {
@@ -163,6 +176,10 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
             copy(static_cast<const S *>(a.y), a.ld_y, r, n % kAhead, 1);
             if (a.dy) copy(static_cast<const S *>(a.dy), a.ld_dy, r, n % kAhead, 2);
             copy(static_cast<const B *>(a.f), a.ld_f, r, n % kAhead, 3);
+            if constexpr (kStage) {
+                if (a.gate.bf16) copy(static_cast<const Bf16 *>(a.gate.p), a.d, r, n % kAhead, 4);
+                else copy(static_cast<const float *>(a.gate.p), a.d, r, n % kAhead, 4);
+            }
         }
         copies_commit();
     };
@@ -277,10 +294,27 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
         for (int q = 0; q < V; ++q) {
             Eight<S> dy;
             Eight<B> f;
-            Pair out[4], each[4], w[4], b[4];
+            Pair out[4], each[4], b[4];
             if (a.dy) take(dy, static_cast<const S *>(a.dy), a.ld_dy, r, live, buffer, q, 2); else dy.zero();
             take(f, static_cast<const B *>(a.f), a.ld_f, r, live, buffer, q, 3);
-            if (kind == kGateElement && live) a.gate.load(cols, r * a.d, q, each);
+            if (ELEMENT && live) {
+                if constexpr (kStage) {
+                    const char *at4 = region(buffer, q, 4);
+                    if (a.gate.bf16) {
+                        Eight<Bf16> g16;
+                        g16.from_shared(at4 + threadIdx.x * 16);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) each[i] = g16.pair(i);
+                    } else {
+                        Eight<float> g32;
+                        g32.from_shared(at4 + threadIdx.x * 32);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) each[i] = g32.pair(i);
+                    }
+                } else {
+                    a.gate.load(cols, r * a.d, q, each);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 Pair s = fma2(t[q][i], by_n, dy.pair(i));
@@ -289,12 +323,11 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
                 out[i] = t[q][i] * Pair(a.residual_scale);
             }
             if (live) cols.store(static_cast<S *>(a.dx) + r * a.ld_dx, q, out);
-            if (kind == kGateElement && live) {
-                a.post_w.load(cols, 0, q, w);
+            if (ELEMENT && live) {
                 if (FULL && a.post_b.p) a.post_b.load(cols, 0, q, b);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    Pair z = normal(f.pair(i), rf, sub_f) * w[i];
+                    Pair z = normal(f.pair(i), rf, sub_f) * through[q][i];
                     if (FULL && a.post_b.p) z = z + b[i];
                     out[i] = t[q][i] * z;
                     t[q][i] = t[q][i] * each[i];                                         // dz
@@ -452,21 +485,26 @@ enum { kPlain, kFull, kEither };
 template <typename S, typename B, int V, int W, int L, int C, bool VEC, int KIND>
 cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaStream_t stream) {
     constexpr int kBlock = kBackThreads<W>;
-    constexpr int kJoin = kBlock * 8 * 4, kLand = VEC ? kRowsAhead<V> * V * static_cast<int>(sizeof(S) + sizeof(B)) * kBlock * 16 : 0;
-    constexpr int kBytes = kLand > kJoin ? kLand : kJoin;
-    if constexpr (kBytes > 220 * 1024) return cudaErrorInvalidValue;      // the plan takes another shape in fp32
+    constexpr int kJoin = kBlock * 8 * 4, kLand = kIncoming<S, B, V, W, VEC>;
+    constexpr int kBytes = kLand > kJoin ? kLand : kJoin, kGate = kStageGate<S, B, V, W, VEC> ? kIncomingGate<V, W> : 0;
+    if constexpr (kBytes > kSharedMost) return cudaErrorInvalidValue;      // the plan takes another shape in fp32
     else {
-    auto kernel = KIND == kFull || (KIND == kEither && p.full) ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain>
-                                                               : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull>;
-    if (kBytes > 40 * 1024) {                          // with the static part, over what needs no asking
-        static std::atomic<uint64_t> done[2];
-        const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kBytes, done[p.full]);
+    const bool element = gate_kind(a) == kGateElement;
+    auto kernel = KIND == kFull || (KIND == kEither && p.full)
+                      ? (element ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain, true>
+                                 : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND != kPlain, false>)
+                      : (element ? peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull, true>
+                                 : peri_backward_kernel<S, B, V, W, L, C, VEC, KIND == kFull, false>);
+    const int bytes = kBytes + (element ? kGate : 0);
+    if (kBytes + kGate > 40 * 1024) {                  // with the static part, over what needs no asking
+        static std::atomic<uint64_t> done[4];
+        const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kernel), kSharedMost, done[2 * element + p.full]);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(static_cast<unsigned>(p.blocks * C));
     config.blockDim = dim3(kBlock);
-    config.dynamicSmemBytes = kBytes;
+    config.dynamicSmemBytes = bytes;
     config.stream = stream;
     cudaLaunchAttribute cluster;
     cluster.id = cudaLaunchAttributeClusterDimension;
