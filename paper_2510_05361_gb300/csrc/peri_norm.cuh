@@ -174,22 +174,21 @@ struct Vector {
     }
     template <bool VEC>
     __device__ __forceinline__ void load(const Columns<VEC> &c, int64_t row, int q, float *x) const {
-        if (VEC && c.valid(q, 0)) {
-            if (bf16) {
-                Eight<Bf16> e;
-                e.load_kept(static_cast<const Bf16 *>(p) + row + c.at(q, 0));
+        if (bf16) {
+            Eight<Bf16> e;
+            if constexpr (!VEC) c.load(static_cast<const Bf16 *>(p) + row, q, e);
+            else if (c.valid(q, 0)) e.load_kept(static_cast<const Bf16 *>(p) + row + c.at(q, 0));
+            else e.zero();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = e.get(i);
-            } else {
-                Eight<float> e;
-                e.load_kept(static_cast<const float *>(p) + row + c.at(q, 0));
+            for (int i = 0; i < 8; ++i) x[i] = e.get(i);
+        } else {
+            Eight<float> e;
+            if constexpr (!VEC) c.load(static_cast<const float *>(p) + row, q, e);
+            else if (c.valid(q, 0)) e.load_kept(static_cast<const float *>(p) + row + c.at(q, 0));
+            else e.zero();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = e.get(i);
-            }
-            return;
+            for (int i = 0; i < 8; ++i) x[i] = e.get(i);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = !VEC && c.valid(q, i) ? get(row + c.at(q, i)) : 0.0f;
     }
 };
 

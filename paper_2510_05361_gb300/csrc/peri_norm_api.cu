@@ -41,7 +41,9 @@ BackwardPlan plan_backward(const NormArgs &a, bool vec) {
     }
     const int threads = p.warps == 3 ? 96 : p.warps <= 4 ? 128 : 32 * p.warps;
     p.groups = threads / (p.warps == 1 ? p.lanes : 32 * p.warps);
-    const int64_t most = kPeriSms * (512 / threads) / p.cluster;
+    // A cluster's thread blocks run in one group of SMs: of four on an SM each no 38 fit, but 36 (more would wait for the
+    // others' end: 4096 fp32 rows of 16384 in 759 us for 465).
+    const int64_t most = (p.cluster == 4 ? 36 : kPeriSms / p.cluster) * (512 / threads);
     p.blocks = std::max<int64_t>(1, std::min(most, (a.rows + p.groups - 1) / p.groups));
     const int64_t workers = p.blocks * p.groups;
     const bool rows_gate = gate_kind(a) == kGateRows;

@@ -332,14 +332,8 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
                     out[i] = t[q][i] * z;
                     t[q][i] = t[q][i] * each[i];                                         // dz
                 }
-                if (VEC) {
-                    if (a.d_gate.bf16) cols.store(static_cast<Bf16 *>(a.d_gate.p) + r * a.d, q, out);
-                    else cols.store(static_cast<float *>(a.d_gate.p) + r * a.d, q, out);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (cols.valid(q, i)) a.d_gate.set(r * a.d + cols.at(q, i), at(out, i));
-                }
+                if (a.d_gate.bf16) cols.store(static_cast<Bf16 *>(a.d_gate.p) + r * a.d, q, out);
+                else cols.store(static_cast<float *>(a.d_gate.p) + r * a.d, q, out);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
