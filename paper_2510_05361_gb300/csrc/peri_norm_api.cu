@@ -26,7 +26,7 @@ BackwardPlan plan_backward(const NormArgs &a, bool vec) {
         p.cluster = a.d <= 4096 ? 1 : 4;
     } else if (a.d <= 256) {
         p.lanes = a.d <= 64 ? 8 : a.d <= 128 ? 16 : 32;
-    } else if (a.d > 4096 && !a.wide) {                // 16 warps and shared memory for two rows of 8192
+    } else if (a.d > 4096 && !a.wide && !p.full) {     // 16 warps and shared memory for two rows of 8192
         p.groups_of_eight = 2;
         p.warps = 16;
         while (8192 * p.cluster < a.d) p.cluster *= 2;

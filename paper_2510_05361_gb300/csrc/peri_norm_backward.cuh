@@ -3,7 +3,7 @@
 // One pass over the rows.  A thread has the same eight or sixteen columns of every row that its worker takes (a
 // worker: the lanes or warps of one row, in one thread block or a cluster of them), so that the sums over rows which
 // the weights' gradients are stay in its registers; a row's own two sums (of the norm before the
-// block, then of the one after it) go over the worker's warps.  The next row is on its way to
+// block, then of the one after it) go over the worker's warps.  The next rows are on their way to
 // shared memory while one is worked on; a warp reads only what it copied itself.
 // Four sums a column: of dh n_y, dh, dY n_f, dY, from which a gate that is the
 // same for the rows summed gives its own gradient and the norm's (post_w S is the gate's, gate S the weight's).
@@ -25,13 +25,13 @@
 namespace mtdao {
 namespace {
 
-template <int W, int L, int G, int C>
+// Sums of N values over a worker's warps.
+template <int W, int L, int G, int C, int N>
 struct RowSums {
-    float parts[G][2][2][W * C];                       // worker's row, use, value
     static constexpr int kWarps = W * C;
+    float parts[G][2][kWarps][N];                      // worker's row, use, warp
 
-    // Sums of N values over the worker's warps; use: 0 and 1 in turn, so that one barrier each is enough.
-    template <int N>
+    // use: 0 and 1 in turn, so that one barrier each is enough.
     __device__ __forceinline__ void add(float (&v)[N], int use) {
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -42,14 +42,16 @@ struct RowSums {
             if constexpr (C > 1) {
                 auto cluster = cooperative_groups::this_cluster();
                 const int rank = static_cast<int>(cluster.block_rank());
+                if (lane < C) {
+                    float *to = cluster.map_shared_rank(parts[group][use][rank * W + warp], lane);
 #pragma unroll
-                for (int n = 0; n < N; ++n)
-                    if (lane < C) *cluster.map_shared_rank(&parts[group][use][n][rank * W + warp], lane) = v[n];
+                    for (int n = 0; n < N; ++n) to[n] = v[n];
+                }
                 cluster.sync();
             } else {
                 if (lane == 0) {
 #pragma unroll
-                    for (int n = 0; n < N; ++n) parts[group][use][n][warp] = v[n];
+                    for (int n = 0; n < N; ++n) parts[group][use][warp][n] = v[n];
                 }
                 if constexpr (G == 1)
                     __syncthreads();
@@ -57,19 +59,23 @@ struct RowSums {
                     asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "n"(32 * W) : "memory");
             }
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                if constexpr (kWarps <= 8) {
-                    v[n] = 0.0f;
+            for (int n = 0; n < N; ++n) v[n] = 0.0f;
+            if constexpr (kWarps <= 8) {
 #pragma unroll
-                    for (int i = 0; i < kWarps; ++i) v[n] += parts[group][use][n][i];
-                } else {
-                    v[n] = 0.0f;
+                for (int i = 0; i < kWarps; ++i)
 #pragma unroll
-                    for (int i = 0; i < kWarps; i += 32)
-                        if (i + lane < kWarps) v[n] += parts[group][use][n][i + lane];
+                    for (int n = 0; n < N; ++n) v[n] += parts[group][use][i][n];
+            } else {
+#pragma unroll
+                for (int i = 0; i < kWarps; i += 32)
+                    if (i + lane < kWarps) {
+#pragma unroll
+                        for (int n = 0; n < N; ++n) v[n] += parts[group][use][i + lane][n];
+                    }
+#pragma unroll
+                for (int n = 0; n < N; ++n)
 #pragma unroll
                     for (int off = 16; off > 0; off >>= 1) v[n] += __shfl_xor_sync(0xffffffffu, v[n], off);
-                }
             }
         }
     }
@@ -96,17 +102,27 @@ template <typename S, typename B, int V, int W, bool VEC>
 constexpr bool kStageGate =
     VEC && V == 1 && (kIncoming<S, B, V, W, VEC> + kIncomingGate<V, W>) * (512 / kBackThreads<W>) <= kSharedMost;
 
+// Whether a row's second sums go over the warps together with the next row's first: one barrier a row instead of two, for
+// reading dh and y from shared memory twice.  It pays with four sums a column: fp32 rows of 2048 go at 91 % of the copy
+// rate for 80, of 1024 at 90 for 83, of 8192 (a cluster's barrier) at 64 for 58; an fp32 stream with a bf16 branch at 91
+// for 81 in rows of 1024, but at 84 for 89 in rows of 2048, so that these keep two.  With two sums a column the second
+// reading costs more than the barrier: bf16 rows of 2048 at 62 for 89.
+template <typename B, int W, int C, bool VEC, bool FULL>
+constexpr bool kJoinSums = VEC && FULL && W > 1 && (sizeof(B) == 4 || W <= 4 || C > 1);
+
 // V groups of eight columns a thread.  FULL: "layer" norm or biases; else the sums of dh and dY and the means are
 // left out.  ELEMENT: a gate for every element (apart: its code costs the others the registers that they need).
 template <typename S, typename B, int V, int W, int L, int C, bool VEC, bool FULL, bool ELEMENT>
 __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_backward_kernel(const NormArgs a) {
-    constexpr int kSums = FULL ? 4 : 2;                 // A, S or A, S, B, D
+    constexpr int kSums = FULL ? 4 : 2, kTwo = kSums / 2;       // A, S or A, S, B, D; a row's sums of one norm
+    constexpr bool kJoin = kJoinSums<B, W, C, VEC, FULL>;
+    constexpr int kValues = kJoin ? 2 * kTwo : kTwo;
     constexpr int kBlock = kBackThreads<W>, kThreads = W == 1 ? L : 32 * W, G = kBlock / kThreads;
     constexpr bool kStage = ELEMENT && kStageGate<S, B, V, W, VEC>;
     constexpr int kRows = static_cast<int>(sizeof(S) + sizeof(B)), kPieces = kRows + (kStage ? 2 : 0);   // of 16 bytes
     constexpr int kAhead = kRowsAhead<V>;
     extern __shared__ __align__(16) char incoming[];    // [kAhead][V][pieces][threads][16]
-    __shared__ RowSums<W, L, G, C> sums;
+    __shared__ __align__(16) RowSums<W, L, G, C, kValues> sums;
     const int group = threadIdx.x / kThreads;
     const int rank = C > 1 ? static_cast<int>(cooperative_groups::this_cluster().block_rank()) : 0;
     const int64_t block = blockIdx.x / C, worker = block * G + group, workers = static_cast<int64_t>(gridDim.x / C) * G;
@@ -246,57 +262,105 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
         if (r < end) next_sy = __ldg(a.stats + a.rows + r), next_sf = __ldg(a.stats + r);
     };
     ask_stats(0);
+    constexpr int kLead = kJoin ? kAhead : kAhead - 1;
 #pragma unroll
-    for (int n = 0; n < kAhead - 1; ++n) fetch(n);
+    for (int n = 0; n < kLead; ++n) fetch(n);
     set_gate(min(first, a.rows - 1));
     int64_t g = kind == kGateRows ? first / a.per_gate : 0, g_end = (g + 1) * a.per_gate;
-    for (int64_t n = 0; n < rounds; ++n) {
+    auto normal = [](Pair z, Pair r, Pair sub) { return FULL ? (z + sub) * r : z * r; };
+    Pair u[V][4], t[V][4];
+    float v[kValues];                                  // the row's first sums; last: its second ones, or (joined) the row's before
+    float *const last = v + (kJoin ? kTwo : 0);
+    // df of row r, whose second sums are there; u: dz times its weight, t: n_f
+    auto finish = [&](int64_t r, float2 sf) {
+        const Pair rf(sf.y), df_n(-sf.y * (last[0] * inv_d)), df_1(FULL && a.layer ? -sf.y * (last[kTwo - 1] * inv_d) : 0.0f);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            Pair out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                out[i] = FULL ? fma2(t[q][i], df_n, df_1) : t[q][i] * df_n;
+                out[i] = fma2(u[q][i], rf, out[i]);
+            }
+            cols.store(static_cast<B *>(a.df) + r * a.ld_df, q, out);
+        }
+        if (kind == kGateRows) {
+            const bool done = r + 1 >= end;
+            if (done || r + 1 == g_end) {
+                end_gate(g);
+                ++g, g_end += a.per_gate;
+                if (!done) set_gate(r + 1);
+            }
+        }
+    };
+    float2 last_sf = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) v[i] = 0.0f;
+    for (int64_t n = 0; n < rounds + (kJoin ? 1 : 0); ++n) {
         const int64_t r = first + n * step;
-        const bool live = r < end;
+        const bool live = n < rounds && r < end;
         const int buffer = n % kAhead;
         const float2 sf = next_sf, sy = next_sy;
-        ask_stats(n + 1);
-        fetch(n + kAhead - 1);
-        copies_wait<kAhead - 1>();
-        __syncwarp();
-        Pair u[V][4], t[V][4], two[FULL ? 2 : 1];
-        two[0] = two[FULL ? 1 : 0] = Pair(0.0f);
         // a normalised value: (z - mean) r (z r - mean r would lose what z and a large mean have in common)
         const Pair ry(sy.y), sub_y(-sy.x), rf(sf.y), sub_f(-sf.x);
-        auto normal = [](Pair z, Pair r, Pair sub) { return FULL ? (z + sub) * r : z * r; };
+        ask_stats(n + 1);
+        if (!kJoin) fetch(n + kLead);
+        copies_wait<kAhead - 1>();
+        __syncwarp();
+        Pair two[kTwo];
+#pragma unroll
+        for (int i = 0; i < kTwo; ++i) two[i] = Pair(0.0f);
+        Eight<S> dy_ahead[VEC ? 1 : V];                // from memory: on their way before the barrier
+        Eight<B> f_ahead[VEC ? 1 : V];
 #pragma unroll
         for (int q = 0; q < V; ++q) {
             Eight<B> dh;
             Eight<S> y;
             take(dh, static_cast<const B *>(a.dh), a.ld_dh, r, live, buffer, q, 0);
             take(y, static_cast<const S *>(a.y), a.ld_y, r, live, buffer, q, 1);
+            if constexpr (!VEC) {
+                take(f_ahead[q], static_cast<const B *>(a.f), a.ld_f, r, live, buffer, q, 3);
+                if (a.dy) take(dy_ahead[q], static_cast<const S *>(a.dy), a.ld_dy, r, live, buffer, q, 2); else dy_ahead[q].zero();
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Pair h = dh.pair(i), m = normal(y.pair(i), ry, sub_y);
-                u[q][i] = h * pre_w[q][i];
-                t[q][i] = m;
-                two[0] = fma2(u[q][i], m, two[0]);
+                const Pair h = dh.pair(i), m = normal(y.pair(i), ry, sub_y), x = h * pre_w[q][i];
+                two[0] = fma2(x, m, two[0]);
                 sum[0][q][i] = fma2(h, m, sum[0][q][i]);
                 if (FULL) {
-                    two[FULL ? 1 : 0] = two[FULL ? 1 : 0] + u[q][i];
+                    two[kTwo - 1] = two[kTwo - 1] + x;
                     sum[FULL ? 2 : 0][q][i] = sum[FULL ? 2 : 0][q][i] + h;
                 }
+                if (!kJoin) u[q][i] = x, t[q][i] = m;
             }
         }
-        float v[FULL ? 2 : 1];
 #pragma unroll
-        for (int i = 0; i < (FULL ? 2 : 1); ++i) v[i] = two[i].lo() + two[i].hi();
-        sums.add(v, 0);
+        for (int i = 0; i < kTwo; ++i) v[i] = two[i].lo() + two[i].hi();
+        sums.add(v, kJoin ? n & 1 : 0);
+        if constexpr (kJoin) {
+            if (n > 0 && r - step < end) finish(r - step, last_sf);
+            if (n == rounds) break;
+        }
         // dY = dy + r (u - n mean(u n) [- mean(u)])
-        const Pair by_n(-sy.y * (v[0] * inv_d)), by_1(FULL && a.layer ? -sy.y * (v[FULL ? 1 : 0] * inv_d) : 0.0f);
-        two[0] = two[FULL ? 1 : 0] = Pair(0.0f);
+        const Pair by_n(-sy.y * (v[0] * inv_d)), by_1(FULL && a.layer ? -sy.y * (v[kTwo - 1] * inv_d) : 0.0f);
+#pragma unroll
+        for (int i = 0; i < kTwo; ++i) two[i] = Pair(0.0f);
 #pragma unroll
         for (int q = 0; q < V; ++q) {
-            Eight<S> dy;
+            Eight<B> dh;
+            Eight<S> y, dy;
             Eight<B> f;
             Pair out[4], each[4], b[4];
-            if (a.dy) take(dy, static_cast<const S *>(a.dy), a.ld_dy, r, live, buffer, q, 2); else dy.zero();
-            take(f, static_cast<const B *>(a.f), a.ld_f, r, live, buffer, q, 3);
+            if (kJoin) {
+                take(dh, static_cast<const B *>(a.dh), a.ld_dh, r, live, buffer, q, 0);
+                take(y, static_cast<const S *>(a.y), a.ld_y, r, live, buffer, q, 1);
+            }
+            if constexpr (!VEC) {
+                dy = dy_ahead[q], f = f_ahead[q];
+            } else {
+                if (a.dy) take(dy, static_cast<const S *>(a.dy), a.ld_dy, r, live, buffer, q, 2); else dy.zero();
+                take(f, static_cast<const B *>(a.f), a.ld_f, r, live, buffer, q, 3);
+            }
             if (ELEMENT && live) {
                 if constexpr (kStage) {
                     const char *at4 = region(buffer, q, 4);
@@ -317,9 +381,10 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                Pair s = fma2(t[q][i], by_n, dy.pair(i));
+                const Pair m = kJoin ? normal(y.pair(i), ry, sub_y) : t[q][i];
+                Pair s = fma2(m, by_n, dy.pair(i));
                 if (FULL) s = s + by_1;
-                t[q][i] = fma2(u[q][i], ry, s);
+                t[q][i] = fma2(kJoin ? dh.pair(i) * pre_w[q][i] : u[q][i], ry, s);
                 out[i] = t[q][i] * Pair(a.residual_scale);
             }
             if (live) cols.store(static_cast<S *>(a.dx) + r * a.ld_dx, q, out);
@@ -343,32 +408,18 @@ __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_b
                 u[q][i] = t[q][i] * through[q][i];
                 t[q][i] = m;
                 two[0] = fma2(u[q][i], m, two[0]);
-                if (FULL) two[FULL ? 1 : 0] = two[FULL ? 1 : 0] + u[q][i];
+                if (FULL) two[kTwo - 1] = two[kTwo - 1] + u[q][i];
             }
         }
 #pragma unroll
-        for (int i = 0; i < (FULL ? 2 : 1); ++i) v[i] = two[i].lo() + two[i].hi();
-        sums.add(v, 1);
-        const Pair df_n(-sf.y * (v[0] * inv_d)), df_1(FULL && a.layer ? -sf.y * (v[FULL ? 1 : 0] * inv_d) : 0.0f);
-        if (live) {
-#pragma unroll
-            for (int q = 0; q < V; ++q) {
-                Pair out[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    out[i] = FULL ? fma2(t[q][i], df_n, df_1) : t[q][i] * df_n;
-                    out[i] = fma2(u[q][i], rf, out[i]);
-                }
-                cols.store(static_cast<B *>(a.df) + r * a.ld_df, q, out);
-            }
-            if (kind == kGateRows) {
-                const bool last = r + 1 == end;
-                if (last || r + 1 == g_end) {
-                    end_gate(g);
-                    ++g, g_end += a.per_gate;
-                    if (!last) set_gate(r + 1);
-                }
-            }
+        for (int i = 0; i < kTwo; ++i) last[i] = two[i].lo() + two[i].hi();
+        if constexpr (kJoin) {
+            last_sf = sf;
+            __syncwarp();                              // the warp has read the buffer
+            fetch(n + kLead);
+        } else {
+            sums.add(v, 1);
+            if (live) finish(r, sf);
         }
     }
     copies_wait<0>();
@@ -479,8 +530,8 @@ enum { kPlain, kFull, kEither };
 template <typename S, typename B, int V, int W, int L, int C, bool VEC, int KIND>
 cudaError_t launch_backward_rows(const NormArgs &a, const BackwardPlan &p, cudaStream_t stream) {
     constexpr int kBlock = kBackThreads<W>;
-    constexpr int kJoin = kBlock * 8 * 4, kLand = kIncoming<S, B, V, W, VEC>;
-    constexpr int kBytes = kLand > kJoin ? kLand : kJoin, kGate = kStageGate<S, B, V, W, VEC> ? kIncomingGate<V, W> : 0;
+    constexpr int kAdd = kBlock * 8 * 4, kLand = kIncoming<S, B, V, W, VEC>;
+    constexpr int kBytes = kLand > kAdd ? kLand : kAdd, kGate = kStageGate<S, B, V, W, VEC> ? kIncomingGate<V, W> : 0;
     if constexpr (kBytes > kSharedMost) return cudaErrorInvalidValue;      // the plan takes another shape in fp32
     else {
     const bool element = gate_kind(a) == kGateElement;
@@ -534,8 +585,8 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
             MTDAO_BACKWARD_CASE(1, 1, 32, 1, true, kEither)
             MTDAO_BACKWARD_CASE(2, 4, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 1, true, kPlain)
-            MTDAO_BACKWARD_CASE(2, 16, 32, 1, true, kEither)
-            MTDAO_BACKWARD_CASE(2, 16, 32, 2, true, kEither)
+            MTDAO_BACKWARD_CASE(2, 16, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 16, 32, 2, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 2, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 4, true, kPlain)
             MTDAO_BACKWARD_CASE(1, 2, 32, 1, true, kEither)
