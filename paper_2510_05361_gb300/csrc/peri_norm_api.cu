@@ -28,11 +28,11 @@ BackwardPlan plan_backward(const NormArgs &a, bool vec) {
         p.lanes = a.d <= 64 ? 8 : a.d <= 128 ? 16 : 32;
     } else if (a.d > 4096 && !a.wide && !p.full) {     // 16 warps and shared memory for two rows of 8192
         p.groups_of_eight = 2;
-        p.warps = 16;
+        p.warps = a.d <= 6144 ? 12 : 16;
         while (8192 * p.cluster < a.d) p.cluster *= 2;
     } else if (p.full || a.d <= 1024) {
         const int need = (a.d + 255) / 256;
-        p.warps = need <= 4 ? need : need <= 8 ? 8 : 16;
+        p.warps = need <= 4 ? need : need <= 8 ? 8 : need > 16 && need <= 24 ? 12 : 16;
         while (4096 * p.cluster < a.d) p.cluster *= 2;
     } else {
         p.groups_of_eight = 2;

@@ -103,19 +103,19 @@ constexpr bool kStageGate =
     VEC && V == 1 && (kIncoming<S, B, V, W, VEC> + kIncomingGate<V, W>) * (512 / kBackThreads<W>) <= kSharedMost;
 
 // Whether a row's second sums go over the warps together with the next row's first: one barrier a row instead of two, for
-// reading dh and y from shared memory twice.  It pays with four sums a column: fp32 rows of 2048 go at 91 % of the copy
-// rate for 80, of 1024 at 90 for 83, of 8192 (a cluster's barrier) at 64 for 58; an fp32 stream with a bf16 branch at 91
-// for 81 in rows of 1024, but at 84 for 89 in rows of 2048, so that these keep two.  With two sums a column the second
-// reading costs more than the barrier: bf16 rows of 2048 at 62 for 89.
-template <typename B, int W, int C, bool VEC, bool FULL>
-constexpr bool kJoinSums = VEC && FULL && W > 1 && (sizeof(B) == 4 || W <= 4 || C > 1);
+// reading dh and y from shared memory twice.  It pays with four sums a column where the barrier is a cluster's (fp32 rows
+// of 8192 go at 64 % of the copy rate for 58, bf16 at 43 for 37) or there are more bytes for each number (fp32 rows of
+// 2048 at 91 for 80; an fp32 stream with a bf16 branch at 91 for 81 in rows of 1024, but 84 for 89 in rows of 2048); not
+// in bf16 (rows of 512 at 68 for 80), nor with two sums (rows of 2048 at 62 for 89).
+template <typename S, typename B, int W, int C, bool VEC, bool FULL>
+constexpr bool kJoinSums = VEC && FULL && W > 1 && (C > 1 || sizeof(B) == 4 || (sizeof(S) == 4 && W <= 4));
 
 // V groups of eight columns a thread.  FULL: "layer" norm or biases; else the sums of dh and dY and the means are
 // left out.  ELEMENT: a gate for every element (apart: its code costs the others the registers that they need).
 template <typename S, typename B, int V, int W, int L, int C, bool VEC, bool FULL, bool ELEMENT>
 __global__ void __launch_bounds__(kBackThreads<W>, 512 / kBackThreads<W>) peri_backward_kernel(const NormArgs a) {
     constexpr int kSums = FULL ? 4 : 2, kTwo = kSums / 2;       // A, S or A, S, B, D; a row's sums of one norm
-    constexpr bool kJoin = kJoinSums<B, W, C, VEC, FULL>;
+    constexpr bool kJoin = kJoinSums<S, B, W, C, VEC, FULL>;
     constexpr int kValues = kJoin ? 2 * kTwo : kTwo;
     constexpr int kBlock = kBackThreads<W>, kThreads = W == 1 ? L : 32 * W, G = kBlock / kThreads;
     constexpr bool kStage = ELEMENT && kStageGate<S, B, V, W, VEC>;
@@ -585,6 +585,7 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
             MTDAO_BACKWARD_CASE(1, 1, 32, 1, true, kEither)
             MTDAO_BACKWARD_CASE(2, 4, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 1, true, kPlain)
+            MTDAO_BACKWARD_CASE(2, 12, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 16, 32, 1, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 16, 32, 2, true, kPlain)
             MTDAO_BACKWARD_CASE(2, 8, 32, 2, true, kPlain)
@@ -594,6 +595,7 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
             MTDAO_BACKWARD_CASE(1, 4, 32, 1, true, kEither)
             MTDAO_BACKWARD_CASE(1, 8, 32, 1, true, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 1, true, kFull)
+            MTDAO_BACKWARD_CASE(1, 12, 32, 2, true, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 2, true, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 4, true, kFull)
             MTDAO_BACKWARD_CASE(1, 1, 32, 1, false, kFull)

@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) peri_forward_kernel(con
         Pair z[R][V][4];
         // mean and reciprocal deviation of the rows that get(n, q, i) gives; at: parts 0 and 1, or 2 and 3
         auto statistics = [&](auto get, float2 (&out)[R], int at) {
-float mean[R] = {}, squares[R];
+            float mean[R] = {}, squares[R];
             if constexpr (LAYER) {
 #pragma unroll
                 for (int n = 0; n < R; ++n) {
@@ -198,6 +198,7 @@ cudaError_t launch_peri_forward(const NormArgs &a, bool vec, cudaStream_t stream
     if (groups <= 6) return launch_forward_rows<S, B, kWide ? 2 : 3, kWide ? 3 : 2, 32, 2, true>(a, stream);
     if (groups <= 8) return launch_forward_rows<S, B, 2, 4, 32, 2, true>(a, stream);
     if (groups <= 16) return launch_forward_rows<S, B, kWide ? 2 : 4, kWide ? 8 : 4, 32, kWide ? 2 : 1, true>(a, stream);
+    if (groups <= 24) return launch_forward_rows<S, B, kWide ? 2 : 3, kWide ? 12 : 8, 32, kWide ? 2 : 1, true>(a, stream);
     if (groups <= 32) return launch_forward_rows<S, B, kWide ? 2 : 4, kWide ? 16 : 8, 32, kWide ? 2 : 1, true>(a, stream);
     return launch_forward_rows<S, B, 4, 16, 32, 1, true>(a, stream);
 }
