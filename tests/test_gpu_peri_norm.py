@@ -100,6 +100,14 @@ CASES = [  # rows, d, norm, stream, branch, weights, bias, gate rows, gate kind,
     (5, 8192, "rms", "f32", "f32", "f32", False, 1, "f32", 0),
     (2, 8193, "layer", "bf16", "bf16", "f32", True, 2, "f32", 0),
     (3, 16384, "layer", "f32", "f32", "f32", True, 1, "f32", 0),
+    (9, 5120, "rms", "bf16", "bf16", "bf16", False, 9, "bf16", 0),
+    (400, 5120, "layer", "f32", "bf16", "f32", True, 5, "f32", 0),
+    (300, 6144, "layer", "f32", "f32", "f32", True, 1, "f32", 8),
+    (160, 8192, "rms", "bf16", "bf16", "f32", False, 0, "f32", 0),
+    (160, 8200, "layer", "bf16", "bf16", "f32", True, 160, "bf16", 0),
+    (90, 16384, "layer", "f32", "bf16", "bf16", True, 3, "f32", 0),
+    (700, 768, "layer", "f32", "bf16", "f32", True, 7, "f32", 0),
+    (1300, 1536, "layer", "f32", "f32", "f32", False, 13, "f32", 0),
     (2000, 40, "layer", "f32", "bf16", "f32", True, 20, "f32", 0),
     (5000, 96, "rms", "bf16", "bf16", "f32", False, 0, "f32", 0),
     (0, 64, "rms", "bf16", "bf16", "f32", False, 0, "f32", 0),
@@ -286,3 +294,25 @@ def test_refusals(P):
             P.mtdao_peri_norm_backward(shape, *a, None, q.data_ptr(), None, x.data_ptr(), h.data_ptr(), w.data_ptr(), None,
                                        q.data_ptr(), None, None, stats.data_ptr(), need - 1)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("d", [8, 72, 136, 264, 520, 776, 1001, 1032, 1544, 2056, 4104, 5120, 6152, 8200])
+@pytest.mark.parametrize("stream,branch", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")])
+def test_columns_past_the_end_hold_nothing(P, d, stream, branch):
+    """Threads past a row's last column: NaN that longer rows left in their place on chip does not reach a result."""
+    whole = 1 << (d - 1).bit_length()
+    for norm, bias, gate in (("layer", True, 304), ("rms", False, 304), ("rms", False, 4)):
+        s = inputs(304, d, stream, branch, "f32", bias, gate, "bf16", seed=d)
+        bad = inputs(304, whole, stream, branch, "f32", bias, gate, "bf16", seed=d)
+        bad = {k: torch.full_like(v, float("nan")) for k, v in bad.items()}
+        results = []
+        for use in (s, bad, s):
+            rest = {k: use.get(k) for k in ("post_bias", "pre_bias", "gate")}
+            y, h, stats = P.peri_norm_forward(use["x"], use["f"], use["post_weight"], use["pre_weight"], **rest, norm=norm,
+                                              save=True)
+            g = P.peri_norm_backward(use["dh"], use["dy"], y, use["f"], stats, use["post_weight"], use["pre_weight"], **rest,
+                                     norm=norm)
+            results.append({"y": y, "h": h, "stats": stats, **g})
+        for k, v in results[0].items():
+            assert torch.isfinite(v).all(), (norm, k)
+            assert torch.equal(v, results[2][k]), (norm, k)
