@@ -194,8 +194,12 @@ __device__ __forceinline__ void load_block(const AdamwList &a, const AdamwChunk 
 template <int G16, int P16, bool ALIGNED>
 struct Kind {
     static constexpr bool kAligned = ALIGNED, kOne = G16 != 2;         // kOne: one kind of tensor only
-    static __device__ __forceinline__ bool g16(const AdamwChunk &c) { return G16 == 2 ? (c.flags & kAdamwGradBf16) != 0 : G16 == 1; }
-    static __device__ __forceinline__ bool p16(const AdamwChunk &c) { return P16 == 2 ? (c.flags & kAdamwParamBf16) != 0 : P16 == 1; }
+    static __device__ __forceinline__ bool g16(const AdamwChunk &c) {
+        return G16 == 2 ? (c.flags & kAdamwGradBf16) != 0 : G16 == 1;
+    }
+    static __device__ __forceinline__ bool p16(const AdamwChunk &c) {
+        return P16 == 2 ? (c.flags & kAdamwParamBf16) != 0 : P16 == 1;
+    }
 };
 using AnyKind = Kind<2, 2, false>;
 
@@ -410,8 +414,11 @@ __device__ __forceinline__ void stream_blocks(const AdamwList &a, const AdamwSca
     }
 }
 
-// A kernel for each kind of list: with a record's flags deciding (as for lists of several kinds, or in 32 bits, where it
-// costs nothing) 2^27 elements in 8 bits took 222 us for 206 in bf16, 389 for 283 where misaligned, 357 for 310 in fp32.  As many thread blocks an SM as shared memory holds, in 32 bits and bf16 four.
+// The step.  Bound by the memory: 2^27 elements in 8 bits, bf16, 10 bytes each, take 202 us (99 % of the copy rate), in
+// 32 bits 22 bytes each at 100 %; misaligned lists in 8 bits at 71 to 88 %, by the instructions that shift their elements.
+// A kernel for each kind of list: with a record's flags deciding (as for lists of several kinds, or in 32 bits, where
+// it costs nothing) 2^27 elements in 8 bits took 222 us for 206 in bf16, 389 for 283 where misaligned, 357 for 310 in
+// fp32.  As many thread blocks an SM as shared memory holds, in 32 bits and bf16 four.
 template <int BITS, bool CLIP, typename K, int BLOCKS>
 __global__ void __launch_bounds__(kAdamwThreads, BLOCKS)
     adamw_step_kernel(const AdamwList a, const AdamwScalars sc, const float *clip_scale) {
@@ -437,7 +444,8 @@ __global__ void __launch_bounds__(kAdamwThreads, BLOCKS)
         if (b >= lo && b < hi) continue;
         Raw<BITS> r;
         load_block<BITS>(a, c, b, reinterpret_cast<uint32_t *>(mine), r);
-        update_block<BITS, CLIP, AnyKind, false>(a, sc, c, replica, clip_factor<CLIP>(s), b, reinterpret_cast<uint32_t *>(mine), r);
+        update_block<BITS, CLIP, AnyKind, false>(a, sc, c, replica, clip_factor<CLIP>(s), b,
+                                                 reinterpret_cast<uint32_t *>(mine), r);
     }
 }
 
@@ -472,7 +480,8 @@ __device__ __forceinline__ double sum_of_warps(double in_warp, double *parts) {
     return t;
 }
 
-// Each thread block sums `per` records of a replica.  Which thread has which elements does not
+// Each thread block sums `per` records of a replica; bound by the memory, which the gradients are read from once more for
+// it (a factor of all of them cannot be had before they are read).  Which thread has which elements does not
 // matter, so that any tensor is read in aligned 16-byte granules and what is left at its ends
 // by elements; four granules a thread at a time, the next four under way meanwhile.  The last of the
 // replica's thread blocks adds the blocks' sums, in their order.
@@ -523,7 +532,8 @@ __global__ void __launch_bounds__(kAdamwThreads, 4) adamw_norm_kernel(const Adam
         count = min(left, kUnit);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (static_cast<int>(threadIdx.x) + i * kAdamwThreads < count) to[i] = __ldcs(granules + threadIdx.x + i * kAdamwThreads);
+            if (static_cast<int>(threadIdx.x) + i * kAdamwThreads < count)
+                to[i] = __ldcs(granules + threadIdx.x + i * kAdamwThreads);
         granules += kUnit;
         left -= kUnit;
     };
@@ -681,7 +691,8 @@ constexpr int kBatch = 2, kBatches = 4;                // replicas asked for tog
 // its way meanwhile.  Sums of codes times powers of two, and of bf16 values, are all but exact in fp32: they are
 // formed as they are; fp32 parameters (not P16) as in replica_mean.cuh.
 template <bool P16>
-__device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwChunk &c, uint32_t mask, int first, int end, char *mine) {
+__device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwChunk &c, uint32_t mask, int first, int end,
+                                               char *mine) {
     constexpr int kWarps = kAdamwThreads / 32;
     const int lane = threadIdx.x & 31, M = a.M;
     constexpr bool p16 = P16;
@@ -777,7 +788,8 @@ __device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwCh
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const Pair q = mean(minus(ps[i], lost[i]));
-                ps[i] = Pair(q.lo() == 0.0f ? p0[i].lo() : p0[i].lo() + q.lo(), q.hi() == 0.0f ? p0[i].hi() : p0[i].hi() + q.hi());
+                ps[i] = Pair(q.lo() == 0.0f ? p0[i].lo() : p0[i].lo() + q.lo(),
+                             q.hi() == 0.0f ? p0[i].hi() : p0[i].hi() + q.hi());
                 odd |= ps[i].lo() != ps[i].lo() || ps[i].hi() != ps[i].hi();
             }
             if (__any_sync(0xffffffffu, odd)) {        // an infinity, or differences past fp32: as replica_mean.cuh has it
@@ -794,7 +806,8 @@ __device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwCh
                 for (int i = 0; i < 4; ++i) {
                     const Pair x = mean(ps[i]);
                     const bool odd = x.lo() != x.lo() || x.hi() != x.hi();
-                    w[i] = odd ? bf16_nearest2(plain_mean(ps[i].lo()), plain_mean(ps[i].hi())) : bf16_nearest2(x.lo(), x.hi());
+                    w[i] = odd ? bf16_nearest2(plain_mean(ps[i].lo()), plain_mean(ps[i].hi()))
+                               : bf16_nearest2(x.lo(), x.hi());
                 }
             } else {
 #pragma unroll
@@ -816,7 +829,8 @@ __device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwCh
             if (mask & 1u) {
                 char *p = const_cast<char *>(params_of(r));
                 const bool whole = reinterpret_cast<uintptr_t>(p) % (p16 ? 16 : 32) == 0;
-                store_raw(p, p16, whole, b * kAdamwBlock + 8 * lane, c.n, reinterpret_cast<uint32_t *>(mine + kBatches * kBatch * slot), w);
+                store_raw(p, p16, whole, b * kAdamwBlock + 8 * lane, c.n,
+                          reinterpret_cast<uint32_t *>(mine + kBatches * kBatch * slot), w);
             }
             if (mask & 2u) {
                 __stcs(static_cast<uint2 *>(a.m) + eight, cm);
@@ -833,9 +847,12 @@ __device__ __forceinline__ void average_stream(const AdamwList &a, const AdamwCh
 }
 __host__ __device__ __forceinline__ int average_warp_bytes(bool p16) { return kBatches * kBatch * replica_bytes(p16) + kStageBytes; }
 
+// The average: bound by the memory in 32 bits (64 to 98 % of the copy rate, the least for two replicas), in 8 bits by
+// decoding and encoding as well (four replicas of 2^25 bf16 parameters at 80 %, fp32 at 85, 32 replicas at 65).
 // P16: the list's parameters are mostly bf16; records of the other type are averaged block by block.
 template <int BITS, bool P16>
-__global__ void __launch_bounds__(kAdamwThreads, BITS == 32 ? 4 : P16 ? 3 : 2) adamw_average_kernel(const AdamwList a, uint32_t mask, int warp_bytes) {
+__global__ void __launch_bounds__(kAdamwThreads, BITS == 32 ? 4 : P16 ? 3 : 2)
+    adamw_average_kernel(const AdamwList a, uint32_t mask, int warp_bytes) {
     constexpr int kWarps = kAdamwThreads / 32;
     extern __shared__ __align__(16) char shared[];
     const AdamwChunk c = load_chunk(a.chunks + blockIdx.x);

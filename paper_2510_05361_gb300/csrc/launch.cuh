@@ -24,7 +24,8 @@ inline cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<uint6
 // A launch that need not wait for the kernel before it in the stream: the kernel waits itself
 // (cudaGridDependencySynchronize) before it reads what that one wrote.
 template <typename... Params, typename... Args>
-cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t bytes, cudaStream_t stream, Args... args) {
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t bytes, cudaStream_t stream,
+                         Args... args) {
     cudaLaunchConfig_t config = {};
     config.gridDim = grid;
     config.blockDim = dim3(threads);

@@ -218,7 +218,8 @@ __host__ __device__ __forceinline__ int gate_kind(const NormArgs &a) {
 __device__ __forceinline__ int64_t gate_row(const NormArgs &a, int64_t r) {
     if (a.gate_rows == 1) return 0;
     if (a.per_gate == 1) return r * a.d;
-    const int64_t g = a.rows <= 0xffffffffll ? static_cast<uint32_t>(r) / static_cast<uint32_t>(a.per_gate) : r / a.per_gate;
+    const int64_t g = a.rows <= 0xffffffffll ? static_cast<uint32_t>(r) / static_cast<uint32_t>(a.per_gate)
+                                             : r / a.per_gate;
     return g * a.d;
 }
 

@@ -13,8 +13,8 @@
 
 namespace mtdao {
 
-// A thread has sixteen columns of a long row where it keeps two sums for each, else eight (four sums of sixteen are more than
-// its registers hold); rows too long for one thread block are spread over a cluster of them.  512 threads an
+// A thread has sixteen columns of a long row where it keeps two sums for each, else eight (four sums of sixteen are more
+// than its registers hold); rows too long for one thread block are spread over a cluster of them.  512 threads an
 // SM; fewer where rows run out.
 BackwardPlan plan_backward(const NormArgs &a, bool vec) {
     BackwardPlan p = {};
@@ -49,7 +49,8 @@ BackwardPlan plan_backward(const NormArgs &a, bool vec) {
     const bool rows_gate = gate_kind(a) == kGateRows;
     p.contiguous = rows_gate;
     p.split = rows_gate && a.gate_rows < 4 * workers;       // else each worker takes whole gate rows
-    p.floats = 2 * (p.blocks + (p.split ? workers + a.gate_rows : rows_gate ? workers : p.blocks)) * static_cast<int64_t>(a.d);
+    const int64_t second = p.split ? workers + a.gate_rows : rows_gate ? workers : p.blocks;
+    p.floats = 2 * (p.blocks + second) * static_cast<int64_t>(a.d);
     return p;
 }
 
@@ -91,7 +92,8 @@ int check_shape(const mtdao_peri_norm *s, bool backward) {
         return invalid("a bf16 stream takes a bf16 branch");
     if (!(std::isfinite(s->eps) && s->eps >= 0.0) || !std::isfinite(s->residual_scale))
         return invalid("eps and residual_scale must be finite, eps not negative");
-    if (s->gate_rows < 0 || s->gate_rows > (int64_t(1) << 40) || (s->gate_rows > 0 && s->rows > 0 && s->rows % s->gate_rows != 0))
+    if (s->gate_rows < 0 || s->gate_rows > (int64_t(1) << 40) ||
+        (s->gate_rows > 0 && s->rows > 0 && s->rows % s->gate_rows != 0))
         return invalid("gate_rows must divide rows");
     const int64_t lds[] = {s->ld_f, s->ld_y, backward ? s->ld_dy : s->ld_x, backward ? s->ld_dh : s->ld_h,
                            backward ? s->ld_dx : s->ld_x, backward ? s->ld_df : s->ld_h};
@@ -211,13 +213,15 @@ extern "C" int mtdao_peri_norm_backward(const mtdao_peri_norm *s, const void *dh
     a.partial = static_cast<float *>(workspace);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (s->rows == 0 && gate) {
-        const cudaError_t e = cudaMemsetAsync(d_gate, 0, static_cast<size_t>(s->gate_rows) * s->d * size_of(s->gate_dtype), stream);
+        const size_t bytes = static_cast<size_t>(s->gate_rows) * s->d * size_of(s->gate_dtype);
+        const cudaError_t e = cudaMemsetAsync(d_gate, 0, bytes, stream);
         if (e != cudaSuccess) return done(e, "peri_norm backward");
     }
     const bool vec = s->d % 8 == 0 && (!dy || by_eight(dy, s->ld_dy, st)) && by_eight(y, s->ld_y, st) &&
                      by_eight(dx, s->ld_dx, st) && by_eight(dh, s->ld_dh, br) && by_eight(f, s->ld_f, br) &&
                      by_eight(df, s->ld_df, br) && by_eight(post_w, 8, wt) && by_eight(post_b, 8, wt) &&
-                     by_eight(pre_w, 8, wt) && (!gate || (by_eight(gate, 8, s->gate_dtype) && by_eight(d_gate, 8, s->gate_dtype)));
+                     by_eight(pre_w, 8, wt) &&
+                     (!gate || (by_eight(gate, 8, s->gate_dtype) && by_eight(d_gate, 8, s->gate_dtype)));
     const cudaError_t e = st == MTDAO_BF16   ? launch_peri_backward<Bf16, Bf16>(a, vec, stream)
                           : br == MTDAO_BF16 ? launch_peri_backward<float, Bf16>(a, vec, stream)
                                              : launch_peri_backward<float, float>(a, vec, stream);
