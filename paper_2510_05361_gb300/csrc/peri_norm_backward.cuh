@@ -7,7 +7,7 @@
 // shared memory while one is worked on; a warp reads only what it copied itself.
 // Bound by the memory where a column has two sums (bf16 rows of 64 to 4096 columns at 69 to 91 % of the copy rate; 2048:
 // 90 %), by the instructions too with four ("layer" norm or biases: fp32 stream, bf16 branch 74 to 92 %, fp32 67 to 91,
-// bf16 58 to 87); longer rows, a thread block or cluster an SM and its barriers, 27 to 81; odd columns 39 to 87.
+// bf16 58 to 87); longer rows, a thread block or cluster an SM and its barriers, 27 to 81; odd columns 19 to 87.
 // Four sums a column: of dh n_y, dh, dY n_f, dY, from which a gate that is the
 // same for the rows summed gives its own gradient and the norm's (post_w S is the gate's, gate S the weight's).
 //
@@ -599,7 +599,9 @@ cudaError_t launch_peri_backward(const NormArgs &args, bool vec, cudaStream_t st
             MTDAO_BACKWARD_CASE(1, 16, 32, 2, true, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 4, true, kFull)
             MTDAO_BACKWARD_CASE(1, 1, 32, 1, false, kFull)
+            MTDAO_BACKWARD_CASE(1, 2, 32, 1, false, kFull)
             MTDAO_BACKWARD_CASE(1, 4, 32, 1, false, kFull)
+            MTDAO_BACKWARD_CASE(1, 8, 32, 1, false, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 1, false, kFull)
             MTDAO_BACKWARD_CASE(1, 16, 32, 4, false, kFull)
 #undef MTDAO_BACKWARD_CASE

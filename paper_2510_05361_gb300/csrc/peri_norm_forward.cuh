@@ -31,7 +31,7 @@ __device__ __forceinline__ void row_sums(float (&v)[R], float (&parts)[R][W]) {
 
 // Bound by the memory: a row's x and f are read and its y and h written, once.  Of the copy rate, rows of 64 to 4096
 // columns: bf16 "rms" 79 to 97 %; "layer" with biases 75 to 97 % on an fp32 stream, 57 to 75 in bf16 (more arithmetic
-// for a byte); rows of 8192 58 to 76, of 16384 46 to 64; rows of odd columns, two or four bytes a load, 25 to 49.
+// for a byte); rows of 8192 58 to 76, of 16384 46 to 64; rows of odd columns, two or four bytes a load, 20 to 73.
 // Rows of up to 8 V columns a thread, over L lanes (W = 1) or W warps.  A thread takes R rows at a time (of few
 // columns; the weights are then read once for all of them); a thread block holds 128 / L or one such set.
 // The rows' loads go out together and the rows stay in registers: they are read and written once.  Thread
@@ -187,7 +187,11 @@ cudaError_t launch_peri_forward(const NormArgs &a, bool vec, cudaStream_t stream
     const int groups = (a.d + 255) / 256;              // of a warp's 256 columns
     if (!vec) {
         if (groups <= 1) return launch_forward_rows<S, B, 1, 1, 32, 1, false>(a, stream);
-        if (groups <= 4) return launch_forward_rows<S, B, 4, 1, 32, 1, false>(a, stream);
+        // few columns a thread, for many warps an SM: rows of 1001 in a warp each took 273 us for 206 (bf16), 335 for 190
+        // (fp32 stream, bf16 branch); of 509 194 for 89 and 266 for 118; of 2001 in four warps 317 for 203 and 445 for 211
+        if (groups <= 2) return launch_forward_rows<S, B, 1, 2, 32, 1, false>(a, stream);
+        if (groups <= 4) return launch_forward_rows<S, B, 2, 2, 32, 1, false>(a, stream);
+        if (groups <= 8) return launch_forward_rows<S, B, 2, 4, 32, 1, false>(a, stream);
         if (groups <= 16) return launch_forward_rows<S, B, 4, 4, 32, 1, false>(a, stream);
         return launch_forward_rows<S, B, 4, 16, 32, 1, false>(a, stream);
     }

@@ -108,6 +108,9 @@ CASES = [  # rows, d, norm, stream, branch, weights, bias, gate rows, gate kind,
     (90, 16384, "layer", "f32", "bf16", "bf16", True, 3, "f32", 0),
     (700, 768, "layer", "f32", "bf16", "f32", True, 7, "f32", 0),
     (1300, 1536, "layer", "f32", "f32", "f32", False, 13, "f32", 0),
+    (1000, 257, "rms", "bf16", "bf16", "f32", False, 8, "f32", 3),
+    (650, 1777, "layer", "f32", "bf16", "f32", True, 13, "bf16", 1),
+    (400, 3001, "layer", "bf16", "bf16", "bf16", True, 1, "bf16", 0),
     (2000, 40, "layer", "f32", "bf16", "f32", True, 20, "f32", 0),
     (5000, 96, "rms", "bf16", "bf16", "f32", False, 0, "f32", 0),
     (0, 64, "rms", "bf16", "bf16", "f32", False, 0, "f32", 0),
@@ -296,7 +299,7 @@ def test_refusals(P):
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("d", [8, 72, 136, 264, 520, 776, 1001, 1032, 1544, 2056, 4104, 5120, 6152, 8200])
+@pytest.mark.parametrize("d", [8, 72, 136, 257, 264, 520, 776, 1001, 1032, 1777, 1544, 2056, 4104, 5120, 6152, 8200])
 @pytest.mark.parametrize("stream,branch", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")])
 def test_columns_past_the_end_hold_nothing(P, d, stream, branch):
     """Threads past a row's last column: NaN that longer rows left in their place on chip does not reach a result."""
@@ -316,3 +319,20 @@ def test_columns_past_the_end_hold_nothing(P, d, stream, branch):
         for k, v in results[0].items():
             assert torch.isfinite(v).all(), (norm, k)
             assert torch.equal(v, results[2][k]), (norm, k)
+
+
+@pytest.mark.parametrize("rows,d,stream,branch", [(400, 3001, "bf16", "bf16"), (300, 1024, "f32", "bf16"), (65, 6144, "f32", "f32")])
+def test_gate_of_every_element_with_biases(P, rows, d, stream, branch):
+    """The gate's gradient dY (post_weight n_f + post_bias) where the two terms may cancel: the bound goes by their magnitudes."""
+    s = inputs(rows, d, stream, branch, branch, True, rows, branch, seed=rows + d)
+    rest = {k: s[k] for k in ("post_bias", "pre_bias", "gate")}
+    y, _, stats = P.peri_norm_forward(s["x"], s["f"], s["post_weight"], s["pre_weight"], **rest, norm="layer", save=True)
+    got = P.peri_norm_backward(s["dh"], s["dy"], y, s["f"], stats, s["post_weight"], s["pre_weight"], **rest, norm="layer")["gate"]
+    dbl = lambda t: t.double().cpu()  # noqa: E731
+    (mf, rf), (my, ry) = ((k[:, :1], k[:, 1:]) for k in dbl(stats))
+    n_y, n_f = (dbl(y) - my) * ry, (dbl(s["f"]) - mf) * rf
+    u = dbl(s["dh"]) * dbl(s["pre_weight"])
+    total = dbl(s["dy"]) + (u - n_y * (u * n_y).mean(1, keepdim=True) - u.mean(1, keepdim=True)) * ry
+    size = u.abs().amax(1, keepdim=True) * ry * (1 + n_y.abs().amax(1, keepdim=True) ** 2) + dbl(s["dy"]).abs().amax(1, keepdim=True)
+    term, bias = n_f * dbl(s["post_weight"]), dbl(s["post_bias"])
+    near(got, total * (term + bias), ("gate", got.dtype), scale=size * (term.abs() + bias.abs()))
